@@ -44,6 +44,18 @@ class MosaicSparseTerm(ctypes.Structure):
                 ("ldd", c_i64)]
 
 
+class MosaicKvCache(ctypes.Structure):
+    _fields_ = [("k", c_ptr), ("v", c_ptr), ("weights", c_ptr), ("order", c_ptr), ("block_table", c_ptr),
+                ("ldt", c_i64), ("pages", c_i64), ("page_stride", c_i64), ("head_stride", c_i64),
+                ("token_stride", c_i64), ("dtype", c_i32), ("batch", c_i32), ("max_blocks", c_i32),
+                ("kv_heads", c_i32), ("head_dim", c_i32), ("page_size", c_i32)]
+
+
+class MosaicRotary(ctypes.Structure):
+    _fields_ = [("table", c_ptr), ("rows", c_i64), ("positions", c_ptr), ("ldp", c_i64), ("naxes", c_i32),
+                ("sections", c_i32 * 4), ("interleaved", c_i32)]
+
+
 # name -> argument types (all return mosaic_status as int32 unless listed)
 _SIGNATURES = {
     "mosaic_abi_version": ([], c_i32),
@@ -80,6 +92,15 @@ _SIGNATURES = {
                                          c_ptr, c_ptr, c_ptr, c_ptr, c_i64, c_ptr], c_i32),
     "mosaic_hadamard_rotate": ([c_ptr, c_i64, c_ptr, c_i64, c_i64, c_i64, c_i64, c_ptr, c_i32, c_ptr], c_i32),
     "mosaic_hadamard28_rotate": ([c_ptr, c_i64, c_ptr, c_i64, c_i64, c_i64, c_ptr, c_i32, c_ptr], c_i32),
+    "mosaic_cache_append": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_i32, c_i64, c_ptr, c_i32,
+                             ctypes.POINTER(MosaicRotary), c_ptr, c_i64, c_ptr, c_ptr, c_ptr], c_i32),
+    "mosaic_cache_attend_workspace": ([ctypes.POINTER(MosaicKvCache), c_i32, c_i64, c_i32, ctypes.POINTER(c_i64)],
+                                      c_i32),
+    "mosaic_cache_attend": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_i32, c_i32, c_ptr, c_i64, ctypes.c_float,
+                             c_i32, c_ptr, c_i64, c_ptr, c_i64, c_ptr], c_i32),
+    "mosaic_cache_evict_workspace": ([ctypes.POINTER(MosaicKvCache), c_i64, c_i64, ctypes.POINTER(c_i64)], c_i32),
+    "mosaic_cache_evict": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_ptr, c_i64, c_i64, c_i64, c_ptr, c_ptr, c_ptr,
+                            c_ptr, c_i64, c_ptr], c_i32),
     "mosaic_probe_mfma_i8": ([c_i32, c_i64, c_ptr, ctypes.POINTER(c_i64), c_ptr], c_i32),
     "mosaic_quantize_rows": ([c_ptr, c_i64, c_i64, c_i64, c_i32, c_ptr, c_i64, c_ptr, c_i64, c_ptr, c_ptr],
                              c_i32),

@@ -1,0 +1,198 @@
+// New tokens into the cache (mosaic_cache_append): rotary positions on several
+// axes and the write of keys and values into their pages, in one pass over the
+// fused q|k|v rows.
+//
+// A pair (x, y) at place p turns into (x c - y s, y c + x s), c and s from the
+// caller's table. One workgroup takes one token: it gathers the token's 2P
+// cosines and sines into LDS once and every head reads them from there, so a
+// row of q|k|v is read once and every output written once.
+#include "cache.h"
+#include "dispatch.h"
+
+namespace mosaic {
+namespace {
+
+// How the elements of a pair lie. A thread works on V consecutive elements
+// (16 bytes of the row).
+enum RotaryMode {
+  ROT_HALVES,         // j and P + j, P a multiple of V: a thread takes both chunks of a pair
+  ROT_HALVES_RAGGED,  // j and P + j, any P: a thread takes one chunk and reads its partners one by one
+  ROT_NEIGHBOURS      // 2j and 2j + 1 (and P = 0, nothing rotated): a chunk holds whole pairs
+};
+
+// The sequence that row t belongs to: the last b < batch with starts[b] <= t.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int64_t t) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (starts[mid] <= t) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// (held, seen) of sequence b after n new tokens.
+__device__ __forceinline__ void advance(const AppendLaunch& a, int b, int32_t n, int64_t slots) {
+  const int64_t held = (int64_t)held_tokens(a.state, b, slots) + n;
+  const int32_t seen = a.state[a.c.batch + b];
+  a.new_state[b] = (int32_t)(held < slots ? held : slots);
+  a.new_state[a.c.batch + b] = (int32_t)((uint32_t)seen + (uint32_t)n);
+}
+
+__device__ __forceinline__ int32_t fresh_tokens(const AppendLaunch& a, int b) {
+  if (a.starts == nullptr) return 1;
+  const int64_t n = (int64_t)a.starts[b + 1] - a.starts[b];
+  return n < 0 ? 0 : n > a.rows ? (int32_t)a.rows : (int32_t)n;
+}
+
+__global__ __launch_bounds__(256) void cache_advance_kernel(AppendLaunch a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b < a.c.batch) advance(a, b, fresh_tokens(a, b), (int64_t)a.c.max_blocks << a.c.log2_page);
+}
+
+template <class T, int V> struct alignas(sizeof(T) * V) Chunk { T e[V]; };
+
+// Where a chunk of a head goes: q_out, or the head's row of k or v.
+template <int XT, int CT, int V>
+__device__ __forceinline__ void store_chunk(const AppendLaunch& a, char* q, int64_t kv_off, bool kept, int head,
+                                            int e0, const float* y) {
+  typedef typename FloatType<XT>::type X;
+  typedef typename FloatType<CT>::type C;
+  const int D = a.c.head_dim;
+  if (head < a.heads) {
+    Chunk<X, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.e[i] = (X)y[i];
+    *(Chunk<X, V>*)(q + ((int64_t)head * D + e0) * sizeof(X)) = o;
+  } else if (kept) {
+    const int h = head - a.heads;
+    const bool value = h >= a.c.kv_heads;
+    Chunk<C, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.e[i] = (C)y[i];
+    char* base = (value ? a.c.v : a.c.k) + kv_off + (value ? h - a.c.kv_heads : h) * a.c.head_stride;
+    *(Chunk<C, V>*)(base + e0 * sizeof(C)) = o;
+  }
+}
+
+template <int XT, int CT, int MODE>
+__global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
+  typedef typename FloatType<XT>::type X;
+  constexpr int V = 16 / sizeof(X);
+  __shared__ float turn[256];                    // cosines of the P pairs, then sines
+  const int64_t t = blockIdx.x;
+  const int threads = blockDim.x, tid = threadIdx.x;
+  const int b = a.starts == nullptr ? (int)t : sequence_of(a.starts, a.c.batch, t);
+  const int32_t i = a.starts == nullptr ? 0 : (int32_t)(t - a.starts[b]);
+  const int64_t slots = (int64_t)a.c.max_blocks << a.c.log2_page;
+  const int64_t slot = (int64_t)held_tokens(a.state, b, slots) + i;
+  const int32_t number = (int32_t)((uint32_t)a.state[a.c.batch + b] + (uint32_t)i);
+  const int32_t page = slot >= 0 && slot < slots ? page_of(a.c, b, slot) : -1;
+  const bool kept = page >= 0;
+  const int64_t kv_off = kept ? row_offset(a.c, page, 0, slot) : 0;
+
+  const int P = a.rot.pairs;
+  for (int j = tid; j < P; j += threads) {
+    const int axis = (j >= a.rot.ends[0]) + (j >= a.rot.ends[1]) + (j >= a.rot.ends[2]);
+    int64_t p = a.rot.positions != nullptr ? a.rot.positions[axis * a.rot.ldp + t] : number;
+    p = p < 0 ? 0 : p >= a.rot.rows ? a.rot.rows - 1 : p;
+    const float* r = a.rot.table + p * 2 * P;
+    turn[j] = r[j];
+    turn[P + j] = r[P + j];
+  }
+  __syncthreads();                               // also: every thread has read the state
+  if (a.starts == nullptr) {
+    if (tid == 0) advance(a, b, 1, slots);       // nobody else reads this sequence's
+  } else if (t == 0 && a.new_state != a.state) {
+    for (int s = tid; s < a.c.batch; s += threads) advance(a, s, fresh_tokens(a, s), slots);
+  }
+  for (int h = tid; kept && h < a.c.kv_heads; h += threads) {
+    const int64_t r = row_index(a.c, page, h, slot);
+    if (a.c.weights != nullptr) a.c.weights[r] = 0.0f;
+    if (a.c.order != nullptr) a.c.order[r] = number;
+  }
+
+  const char* x = (const char*)a.x + t * a.ldx;
+  char* q = (char*)a.q + t * a.ldq;
+  const int D = a.c.head_dim, chunks = D / V, pc = MODE == ROT_HALVES ? P / V : 0;
+  const int turned_heads = a.heads + a.c.kv_heads;
+  const int per_turned = chunks - pc;            // units of a rotated head; a value head has `chunks`
+  const int units = turned_heads * per_turned + a.c.kv_heads * chunks;
+  for (int u = tid; u < units; u += threads) {
+    const bool turned = u < turned_heads * per_turned;
+    const int w = turned ? u : u - turned_heads * per_turned;
+    const int per = turned ? per_turned : chunks;
+    const int head = w / per + (turned ? 0 : turned_heads), r = w - (w / per) * per;
+    const char* xh = x + (int64_t)head * D * sizeof(X);
+    const int e0 = V * (MODE == ROT_HALVES && turned && r >= pc ? r + pc : r);
+    float v[V], y[V];
+    {
+      const Chunk<X, V> c = *(const Chunk<X, V>*)(xh + e0 * sizeof(X));
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = y[k] = (float)c.e[k];
+    }
+    if (turned && MODE == ROT_HALVES && r < pc) {
+      const Chunk<X, V> c = *(const Chunk<X, V>*)(xh + (e0 + P) * sizeof(X));
+      float z[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float o = (float)c.e[k], cs = turn[e0 + k], sn = turn[P + e0 + k];
+        y[k] = v[k] * cs - o * sn;
+        z[k] = o * cs + v[k] * sn;
+      }
+      store_chunk<XT, CT, V>(a, q, kv_off, kept, head, e0 + P, z);
+    } else if (turned && MODE == ROT_HALVES_RAGGED) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int e = e0 + k;
+        if (e < 2 * P) {
+          const int j = e < P ? e : e - P;
+          const float o = (float)((const X*)xh)[e < P ? e + P : e - P];
+          y[k] = e < P ? v[k] * turn[j] - o * turn[P + j] : v[k] * turn[j] + o * turn[P + j];
+        }
+      }
+    } else if (turned && MODE == ROT_NEIGHBOURS) {
+#pragma unroll
+      for (int k = 0; k < V; k += 2) {
+        const int j = (e0 + k) / 2;
+        if (j < P) {
+          y[k] = v[k] * turn[j] - v[k + 1] * turn[P + j];
+          y[k + 1] = v[k + 1] * turn[j] + v[k] * turn[P + j];
+        }
+      }
+    }
+    store_chunk<XT, CT, V>(a, q, kv_off, kept, head, e0, y);
+  }
+}
+
+template <int XT, int CT>
+void launch_mode(const AppendLaunch& a, hipStream_t s) {
+  constexpr int V = XT == MOSAIC_F32 ? 4 : 8;
+  const dim3 grid((unsigned)a.rows), block(256);
+  if (a.rot.pairs == 0 || a.rot.interleaved) cache_append_kernel<XT, CT, ROT_NEIGHBOURS><<<grid, block, 0, s>>>(a);
+  else if (a.rot.pairs % V == 0) cache_append_kernel<XT, CT, ROT_HALVES><<<grid, block, 0, s>>>(a);
+  else cache_append_kernel<XT, CT, ROT_HALVES_RAGGED><<<grid, block, 0, s>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const AppendLaunch& a, hipStream_t s) {
+  if (a.rows > 0) {
+    if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_F32) launch_mode<MOSAIC_F32, MOSAIC_F32>(a, s);
+    else if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_BF16) launch_mode<MOSAIC_F32, MOSAIC_BF16>(a, s);
+    else if (a.x_dtype == MOSAIC_F32) launch_mode<MOSAIC_F32, MOSAIC_F16>(a, s);
+    else if (a.c.dtype == MOSAIC_BF16) launch_mode<MOSAIC_BF16, MOSAIC_BF16>(a, s);
+    else launch_mode<MOSAIC_F16, MOSAIC_F16>(a, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  // the workgroups above read the state of a sequence in any order, so one
+  // that is written in place waits for the last of them
+  if (a.starts != nullptr && (a.rows == 0 || a.new_state == a.state)) {
+    cache_advance_kernel<<<(a.c.batch + 255) / 256, 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace mosaic

@@ -515,6 +515,220 @@ def mosaic_quantize_rows(x: torch.Tensor, qmax: int, q: Optional[torch.Tensor] =
                                             _ptr(scale), _stream()), "mosaic_quantize_rows")
 
 
+@dataclass
+class KVCache:
+    """Keys and values of a batch of sequences in pages (include/mosaic_cache.h).
+
+    ``k`` and ``v`` have shape (pages, kv_heads, page_size, head_dim) and the
+    same strides, with contiguous rows: a view of memory that is laid out
+    (pages, page_size, kv_heads, head_dim) will do. ``block_table`` (int32,
+    batch x blocks) holds every sequence's pages, ``state`` (int32, 2 x batch)
+    how many tokens it holds and how many it has seen. ``weights`` (float32)
+    and ``order`` (int32), contiguous (pages, kv_heads, page_size), are needed
+    for eviction only."""
+    k: torch.Tensor
+    v: torch.Tensor
+    block_table: torch.Tensor
+    state: torch.Tensor
+    weights: Optional[torch.Tensor] = None
+    order: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def empty(batch: int, max_len: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, page_size: int = 64,
+              evicts: bool = False, device="cuda") -> "KVCache":
+        """A cache without tokens, with pages of its own for ``max_len`` slots
+        of each sequence."""
+        blocks = (max_len + page_size - 1) // page_size
+        pages = batch * blocks
+        k = torch.empty((pages, kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        table = torch.arange(pages, dtype=torch.int32, device=device).reshape(batch, blocks)
+        state = torch.zeros((2, batch), dtype=torch.int32, device=device)
+        weights = torch.zeros(k.shape[:3], device=device) if evicts else None
+        order = torch.zeros(k.shape[:3], dtype=torch.int32, device=device) if evicts else None
+        return KVCache(k, torch.empty_like(k), table, state, weights, order)
+
+    @property
+    def batch(self) -> int:
+        return self.block_table.shape[0]
+
+    @property
+    def slots(self) -> int:
+        """Tokens that a sequence's block table has room for."""
+        return self.block_table.shape[1] * self.k.shape[2]
+
+
+@dataclass
+class Rotary:
+    """Rotary positions: ``table`` (float32, rows x 2P) holds cosines and sines
+    by place and pair, ``sections`` the pairs of each axis (their sum is P),
+    ``positions`` (int32, axes x tokens) each new token's places; None: its
+    number in its sequence. Pairs are the elements j and P + j of a head, or
+    2j and 2j + 1 if ``interleaved``."""
+    table: torch.Tensor
+    sections: Sequence[int]
+    positions: Optional[torch.Tensor] = None
+    interleaved: bool = False
+
+    @staticmethod
+    def frequencies(rows: int, pairs: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+        """The table of angles place * base^(-j / pairs), from float64."""
+        f = base ** (-torch.arange(pairs, dtype=torch.float64, device=device) / pairs)
+        a = torch.arange(rows, dtype=torch.float64, device=device)[:, None] * f
+        return torch.cat([a.cos(), a.sin()], dim=1).float()
+
+
+_FTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _device_tensor(t, name: str, dtypes, dim: int) -> None:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {tuple(dtypes)}")
+    if t.dim() != dim:
+        raise ValueError(f"{name} must have {dim} dimensions")
+
+
+def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
+    """The C struct of a cache whose tensors fit together."""
+    k, v, table = cache.k, cache.v, cache.block_table
+    _device_tensor(k, "cache.k", _FTYPE, 4)
+    _device_tensor(v, "cache.v", _FTYPE, 4)
+    if v.dtype != k.dtype or v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("cache.k and cache.v must have the same type, shape and strides")
+    if k.stride(3) != 1:
+        raise ValueError("rows of cache.k and cache.v must be contiguous")
+    _device_tensor(table, "cache.block_table", _INT, 2)
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("rows of cache.block_table must be contiguous")
+    batch, blocks = table.shape
+    _device_tensor(cache.state, "cache.state", _INT, 2)
+    if tuple(cache.state.shape) != (2, batch) or not cache.state.is_contiguous():
+        raise ValueError("cache.state must be a contiguous (2, batch) tensor")
+    for name, t, dt in (("weights", cache.weights, torch.float32), ("order", cache.order, torch.int32)):
+        if t is not None:
+            _device_tensor(t, f"cache.{name}", (dt,), 3)
+            if t.shape != k.shape[:3] or not t.is_contiguous():
+                raise ValueError(f"cache.{name} must be a contiguous (pages, kv_heads, page_size) tensor")
+    pages, heads, page, dim = k.shape
+    return _lib.MosaicKvCache(k=_ptr(k), v=_ptr(v), weights=_ptr(cache.weights), order=_ptr(cache.order),
+                              block_table=_ptr(table), ldt=max(table.stride(0), blocks), pages=pages,
+                              page_stride=k.stride(0), head_stride=k.stride(1), token_stride=k.stride(2),
+                              dtype=_FTYPE[k.dtype], batch=batch, max_blocks=blocks, kv_heads=heads, head_dim=dim,
+                              page_size=page)
+
+
+def _cache_rows(t: torch.Tensor, rows: int, cols: int, name: str, cache: KVCache) -> None:
+    _device_tensor(t, name, (torch.float32, cache.k.dtype), 2)
+    if t.shape[0] < rows or t.shape[1] < cols:
+        raise ValueError(f"{name} is {tuple(t.shape)}, needs at least ({rows}, {cols})")
+    if t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+
+
+def _same_shape(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: str) -> Optional[torch.Tensor]:
+    if t is None:
+        return like
+    if like is None:
+        raise ValueError(f"{name} has no counterpart in the cache")
+    _device_tensor(t, name, (like.dtype,), like.dim())
+    if t.shape != like.shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(like.shape)} tensor")
+    return t
+
+
+def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Tensor,
+                        starts: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                        new_state: Optional[torch.Tensor] = None) -> None:
+    """New tokens, one per row of qkv (queries, keys, values of ``heads`` and
+    kv_heads heads): rotated queries to q_out, rotated keys and values into
+    the cache. Rows starts[b] .. starts[b + 1] - 1 are sequence b's (None: row
+    b). The state is advanced in place unless new_state is given."""
+    c = _cache_arg(cache)
+    rows = qkv.shape[0]
+    _cache_rows(qkv, rows, (heads + 2 * c.kv_heads) * c.head_dim, "qkv", cache)
+    _cache_rows(q_out, rows, heads * c.head_dim, "q_out", cache)
+    if q_out.dtype != qkv.dtype:
+        raise ValueError("q_out must have the type of qkv")
+    if starts is not None:
+        _device_tensor(starts, "starts", _INT, 1)
+        if starts.shape[0] != c.batch + 1 or starts.stride(0) != 1:
+            raise ValueError("starts must be a contiguous vector of batch + 1 entries")
+    state = _same_shape(new_state, cache.state, "new_state")
+    r = None
+    if rotary is not None:
+        sections = [int(n) for n in rotary.sections]
+        if not 1 <= len(sections) <= 4:
+            raise ValueError("rotary positions have one to four axes")
+        _device_tensor(rotary.table, "rotary.table", (torch.float32,), 2)
+        if rotary.table.shape[1] != 2 * sum(sections) or not rotary.table.is_contiguous():
+            raise ValueError("rotary.table must be contiguous, with a cosine and a sine for every pair")
+        if rotary.positions is not None:
+            _device_tensor(rotary.positions, "rotary.positions", _INT, 2)
+            if rotary.positions.shape[0] < len(sections) or rotary.positions.shape[1] < rows or \
+                    rotary.positions.stride(1) != 1:
+                raise ValueError("rotary.positions must hold a row of places for every axis")
+        r = _lib.MosaicRotary(table=_ptr(rotary.table), rows=rotary.table.shape[0], positions=_ptr(rotary.positions),
+                              ldp=0 if rotary.positions is None else max(rotary.positions.stride(0), rows),
+                              naxes=len(sections), sections=(ctypes.c_int32 * 4)(*sections),
+                              interleaved=1 if rotary.interleaved else 0)
+    _check(_lib.load().mosaic_cache_append(ctypes.byref(c), _ptr(qkv), qkv.stride(0), _FTYPE[qkv.dtype], rows,
+                                           _ptr(starts), heads, None if r is None else ctypes.byref(r), _ptr(q_out),
+                                           q_out.stride(0), _ptr(cache.state), _ptr(state), _stream()),
+           "mosaic_cache_append")
+
+
+def mosaic_cache_attend(cache: KVCache, q: torch.Tensor, heads: int, out: torch.Tensor,
+                        max_len: Optional[int] = None, scale: Optional[float] = None,
+                        accumulate: bool = False) -> None:
+    """out[b] = attention of q[b] (one new token, ``heads`` heads) over the
+    tokens that sequence b holds; ``accumulate`` adds the attention weights
+    up in cache.weights. ``max_len``: no sequence holds more tokens (None: as
+    many as there are slots). ``scale`` defaults to 1 / sqrt(head_dim)."""
+    c = _cache_arg(cache)
+    _cache_rows(q, c.batch, heads * c.head_dim, "q", cache)
+    _cache_rows(out, c.batch, heads * c.head_dim, "out", cache)
+    if out.dtype != q.dtype:
+        raise ValueError("out must have the type of q")
+    if accumulate and cache.weights is None:
+        raise ValueError("the cache has no weights to add to")
+    n = cache.slots if max_len is None else max_len
+    lib, size = _lib.load(), ctypes.c_int64(0)
+    _check(lib.mosaic_cache_attend_workspace(ctypes.byref(c), heads, n, 1 if accumulate else 0, ctypes.byref(size)),
+           "mosaic_cache_attend_workspace")
+    work = torch.empty(size.value, dtype=torch.uint8, device=q.device)
+    _check(lib.mosaic_cache_attend(ctypes.byref(c), _ptr(q), q.stride(0), _FTYPE[q.dtype], heads, _ptr(cache.state), n,
+                                   c.head_dim ** -0.5 if scale is None else scale, 1 if accumulate else 0, _ptr(out),
+                                   out.stride(0), _ptr(work), size.value, _stream()), "mosaic_cache_attend")
+
+
+def mosaic_cache_evict(cache: KVCache, budget: int, recent: int, max_len: Optional[int] = None,
+                       new_state: Optional[torch.Tensor] = None, new_weights: Optional[torch.Tensor] = None,
+                       new_order: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None) -> None:
+    """Every sequence that holds more than ``budget`` tokens keeps, for each
+    key/value head, the ``recent`` latest and the ones with the largest
+    weights, moved into its first ``budget`` slots. Weights, order and state
+    change in place unless others are given; ``kept`` (int32, batch x kv_heads
+    x budget) gets the slot that each slot's token had before."""
+    c = _cache_arg(cache)
+    if cache.weights is None or cache.order is None:
+        raise ValueError("eviction needs a cache with weights and order")
+    state = _same_shape(new_state, cache.state, "new_state")
+    weights = _same_shape(new_weights, cache.weights, "new_weights")
+    order = _same_shape(new_order, cache.order, "new_order")
+    if kept is not None:
+        _device_tensor(kept, "kept", _INT, 3)
+        if tuple(kept.shape) != (c.batch, c.kv_heads, budget) or not kept.is_contiguous():
+            raise ValueError("kept must be a contiguous (batch, kv_heads, budget) tensor")
+    n = cache.slots if max_len is None else max_len
+    lib, size = _lib.load(), ctypes.c_int64(0)
+    _check(lib.mosaic_cache_evict_workspace(ctypes.byref(c), n, budget, ctypes.byref(size)),
+           "mosaic_cache_evict_workspace")
+    work = torch.empty(size.value, dtype=torch.uint8, device=cache.k.device)
+    _check(lib.mosaic_cache_evict(ctypes.byref(c), _ptr(cache.state), _ptr(state), n, budget, recent, _ptr(weights),
+                                  _ptr(order), _ptr(kept), _ptr(work), size.value, _stream()), "mosaic_cache_evict")
+
+
 def mosaic_probe_mfma_i8(mode: int, iters: int, out: torch.Tensor) -> int:
     """Launches the register-only MFMA probe (measurement aid); returns the
     int8 operations launched. ``out`` is a one-element int32 device tensor."""

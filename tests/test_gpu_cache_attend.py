@@ -1,0 +1,287 @@
+"""Attention of one new token over a paged cache, against the float64 oracle.
+
+Tolerance of an output of head g, from the formulas: a score is a float32 sum
+of dim products, off by at most (dim + 4) u S, S the largest sum of |q k|
+scale over the tokens and u = 2^-24; a softmax weight is then off by twice
+that (its own score and the sum's) and its sum over n tokens by n u, all
+relative, so an output by (2 (dim + 4) S + n + 16) u A, A = sum p |v|. With
+16-bit activations the weights are rounded to 16 bits before the product with
+the values (one more unit of that type times A); the output is rounded once.
+A weight added up in the cache carries the same relative error."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as oc
+from paper_2607_29221_amd import mosaic as m
+from tests.cache_util import DT, TINY, TYPES, UNIT, clone, f64, get, make_cache, put, same_bits, seeded
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def check(c, q, heads, out, act, scale, before=None, holes=(), max_len=None):
+    """out (and c.weights, if ``before`` holds what they were) against the oracle;
+    ``holes``: (sequence, block) pairs that the table does not have."""
+    KV, page, D = c.k.shape[1], c.k.shape[2], c.k.shape[3]
+    G = heads // KV
+    lengths = c.state[0].tolist()
+    got, qs = f64(out).reshape(-1, heads, D), f64(q).reshape(-1, heads, D)
+    for b, n in enumerate(lengths):
+        n = max(0, min(n, c.slots if max_len is None else max_len))
+        there = np.ones(n, dtype=bool)
+        for s, j in holes:
+            if s == b:
+                there[j * page: (j + 1) * page] = False
+        if n == 0 or not there.any():
+            assert not got[b].any()
+            continue
+        k, v = get(c, "k", b, n)[:, there], get(c, "v", b, n)[:, there]
+        for h in range(KV):
+            o, p = oc.attend(qs[b, h * G: (h + 1) * G], k[h], v[h], scale)
+            S = abs(scale) * (np.abs(qs[b, h * G: (h + 1) * G]) @ np.abs(k[h]).T).max(axis=1, keepdims=True)
+            A = p @ np.abs(v[h])
+            rel = (2 * (D + 4) * S + n + 16) * U
+            tol = (rel + (UNIT[act] if act != "f32" else 0.0)) * A + UNIT[act] * np.abs(o) + TINY[act]
+            err = np.abs(got[b, h * G: (h + 1) * G] - o)
+            assert (err <= tol).all(), (b, h, err.max(), tol[err > tol][:3])
+            if before is not None:
+                want = before[b][h][there] + p.sum(axis=0)
+                now = get(c, "weights", b, n)[h][there]
+                assert (np.abs(now - want) <= (rel * p).sum(axis=0) + 4 * U * want + 1e-38).all()
+
+
+def run(c, heads, act, seed, accumulate=False, scale=None, std=1.0, **kw):
+    D = c.k.shape[3]
+    q = (torch.randn((c.batch, heads * D), generator=seeded(seed), device="cuda") * std).to(DT[act])
+    out = torch.full_like(q, float("nan"))
+    m.mosaic_cache_attend(c, q, heads, out, scale=scale, accumulate=accumulate, **kw)
+    return q, out, 1.0 / math.sqrt(D) if scale is None else scale
+
+
+LENGTHS = ((1,), (0, 1, 2, 15, 16, 17, 31, 32, 33), (63, 64, 65, 127, 129, 0, 300), (2047, 1025))
+# (heads, kv_heads, dim)
+SHAPES = ((4, 2, 64), (8, 1, 128), (6, 6, 128), (6, 2, 80), (10, 2, 8), (33, 1, 64), (3, 3, 256), (14, 2, 104),
+          (5, 1, 40))
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda v: f"len{max(v)}")
+def test_attend(act, cache, heads, kv, dim, lengths):
+    c = make_cache(lengths, kv, dim, 16 if max(lengths) < 100 else 64, cache, 11, layout="tokens" if dim == 80 else "heads")
+    q, out, scale = run(c, heads, act, 12)
+    check(c, q, heads, out, act, scale)
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", ((4, 2, 64), (8, 1, 128), (40, 2, 80), (3, 3, 256)))
+@pytest.mark.parametrize("page", (16, 32, 128))
+def test_weights_add_up(act, cache, heads, kv, dim, page):
+    """Two steps in a row; weights of other slots stay as they are."""
+    lengths = (0, 1, 77, 513)
+    c = make_cache(lengths, kv, dim, page, cache, 21, evicts=True, layout="tokens" if page == 32 else "heads")
+    for step in range(2):
+        old = clone(c)
+        before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+        q, out, scale = run(c, heads, act, 22 + step, accumulate=True)
+        check(c, q, heads, out, act, scale, before)
+        used = torch.zeros_like(c.weights, dtype=torch.bool)
+        for b, n in enumerate(lengths):
+            i = torch.arange(n, device="cuda")
+            used[c.block_table[b].long()[i // page], :, i % page] = True
+        assert same_bits(c.weights[~used], old.weights[~used])
+        assert same_bits(c.k, old.k) and same_bits(c.v, old.v) and torch.equal(c.state, old.state)
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_long_sequences(act, cache):
+    """Work split over the length: one sequence of many tokens beside short ones."""
+    c = make_cache((20001, 3, 0, 4097), 2, 128, 64, cache, 31, evicts=True)
+    before = [get(c, "weights", b, n) for b, n in enumerate(c.state[0].tolist())]
+    q, out, scale = run(c, 16, act, 32, accumulate=True, std=3.0)
+    check(c, q, 16, out, act, scale, before)
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("std", (0.0, 30.0, 300.0))
+def test_sharp_and_flat(act, cache, std):
+    """All scores alike, and scores so far apart that one token has all the weight."""
+    c = make_cache((1, 500, 37), 2, 64, 32, cache, 41, evicts=True)
+    before = [get(c, "weights", b, n) for b, n in enumerate(c.state[0].tolist())]
+    q, out, scale = run(c, 4, act, 42, accumulate=True, std=std)
+    check(c, q, 4, out, act, scale, before)
+
+
+@pytest.mark.parametrize("act,cache", (("f32", "f16"), ("f16", "f16")))
+def test_large_and_small_halves(act, cache):
+    """Queries near the ends of the 16-bit range."""
+    for std, scale in ((8000.0, 1e-5), (1e-4, 2000.0)):
+        c = make_cache((5, 200), 1, 64, 16, cache, 45)
+        q, out, scale = run(c, 4, act, 46, std=std, scale=scale)
+        check(c, q, 4, out, act, scale)
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("scale", (-0.3, 0.0, 2.0))
+def test_scale(act, cache, scale):
+    c = make_cache((70, 5), 2, 64, 16, cache, 51)
+    q, out, _ = run(c, 4, act, 52, scale=scale)
+    check(c, q, 4, out, act, scale)
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_pages_that_are_not_there(act, cache):
+    """Entries outside the pool: their tokens are left out; a sequence of
+    nothing else gives zeros."""
+    lengths, holes = (100, 40, 16, 333), ((0, 0), (0, 3), (1, 2), (2, 0), (3, 5), (3, 6), (3, 20))
+    c = make_cache(lengths, 2, 64, 16, cache, 61, evicts=True)
+    whole = clone(c)
+    for n, (b, j) in enumerate(holes):
+        c.block_table[b, j] = (-1, c.k.shape[0], 2 ** 31 - 1, -(2 ** 31))[n % 4]
+    before = [get(whole, "weights", b, n) for b, n in enumerate(lengths)]
+    q, out, scale = run(c, 4, act, 62, accumulate=True)
+    c.block_table.copy_(whole.block_table)                  # to read the pages for the check
+    check(c, q, 4, out, act, scale, before, holes)
+    for b, j in holes:
+        p = int(c.block_table[b, j])
+        assert same_bits(c.weights[p], whole.weights[p])
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_lengths_are_bounded(act, cache):
+    """Negative lengths, lengths beyond the table and beyond max_len."""
+    c = make_cache((64, 64, 64), 2, 64, 16, cache, 71)
+    c.state[0] = torch.tensor([-5, 1 << 30, 50], dtype=torch.int32, device="cuda")
+    q, out, scale = run(c, 4, act, 72)
+    check(c, q, 4, out, act, scale)
+    q, out, scale = run(c, 4, act, 73, max_len=37)
+    check(c, q, 4, out, act, scale, max_len=37)
+    q, out, scale = run(c, 4, act, 74, max_len=0)
+    assert not out.any()
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_infinities_in_empty_places(act, cache):
+    """What lies behind the last token never shows, whatever it is."""
+    outs = []
+    for junk in (0.0, float("inf"), float("-inf"), float("nan"), torch.finfo(DT[cache]).min):
+        c = make_cache((1, 30, 100), 2, 80, 32, cache, 81, junk=junk, gap=16)
+        outs.append(run(c, 4, act, 82)[1])
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+def test_strided_rows():
+    """Queries and outputs as columns of wider matrices, a table wider than its
+    sequences, every other page of a pool of keys and values."""
+    base = make_cache((40, 97), 2, 64, 16, "bf16", 91)
+    P, D = base.k.shape[0], 64
+    pool = torch.full((P, 2, 2, 16, D + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    pool[:, 0, :, :, :D], pool[:, 1, :, :, :D] = base.k, base.v
+    wide = torch.full((2, 20), -1, dtype=torch.int32, device="cuda")
+    blocks = base.block_table.shape[1]
+    wide[:, 3: 3 + blocks] = base.block_table
+    c = m.KVCache(pool[:, 0, :, :, :D], pool[:, 1, :, :, :D], wide[:, 3: 3 + blocks], base.state)
+    q = torch.randn((2, 6 * D), generator=seeded(92), device="cuda")
+    out = torch.zeros((2, 8 * D), device="cuda")
+    m.mosaic_cache_attend(c, q[:, D: 5 * D], 4, out[:, 2 * D: 6 * D])
+    check(base, q[:, D: 5 * D], 4, out[:, 2 * D: 6 * D], "f32", D ** -0.5)
+    assert not out[:, : 2 * D].any() and not out[:, 6 * D:].any()
+
+
+@pytest.mark.parametrize("act,cache", (("f32", "bf16"), ("f16", "f16"), ("f32", "f32")))
+def test_same_bits_every_time(act, cache):
+    """No sum depends on the order in which workgroups finish."""
+    c = make_cache((3000, 50, 9000), 2, 64, 32, cache, 101, evicts=True)
+    first = clone(c)
+    _, a, _ = run(c, 8, act, 102, accumulate=True)
+    for _ in range(3):
+        again = clone(first)
+        _, o, _ = run(again, 8, act, 102, accumulate=True)
+        assert torch.equal(a, o) and same_bits(again.weights, c.weights)
+
+
+def test_side_stream_and_graph():
+    """On a stream of its own, and captured: every replay equals the eager call."""
+    c = make_cache((700, 20, 1500), 2, 128, 64, "bf16", 111, evicts=True)
+    want = clone(c)
+    q = torch.randn((3, 16 * 128), generator=seeded(112), device="cuda")
+    expected = []
+    out = torch.empty_like(q)
+    for _ in range(5):
+        m.mosaic_cache_attend(want, q, 16, out, accumulate=True)
+        expected.append((out.clone(), want.weights.clone()))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        m.mosaic_cache_attend(c, q, 16, out, accumulate=True)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(out, expected[0][0]) and same_bits(c.weights, expected[0][1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.mosaic_cache_attend(c, q, 16, out, accumulate=True)
+    for o, w in expected[1:]:
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, o) and same_bits(c.weights, w)
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_far_pages():
+    """Pages whose offsets pass 32 bits."""
+    D, page, pages = 128, 64, 1 << 15
+    big = torch.empty((pages, 8, page, D), dtype=torch.bfloat16, device="cuda")     # 4.3 GB
+    c = make_cache((200,), 8, D, page, "bf16", 121)
+    far = torch.tensor([pages - 1, 5, pages - 2, 16385], device="cuda")
+    v = torch.empty_like(big)
+    big[far], v[far] = c.k[c.block_table[0].long()], c.v[c.block_table[0].long()]
+    f = m.KVCache(big, v, far.to(torch.int32)[None, :], c.state)
+    _, a, _ = run(c, 16, "bf16", 122)
+    _, b, _ = run(f, 16, "bf16", 122)
+    assert torch.equal(a, b)
+
+
+def test_empty_batch():
+    c = make_cache((), 2, 64, 16, "bf16", 131)
+    q = torch.empty((0, 256), device="cuda")
+    m.mosaic_cache_attend(c, q, 4, torch.empty_like(q))
+
+
+def test_refusals():
+    c = make_cache((40,), 2, 64, 16, "bf16", 141)
+    q = torch.zeros((1, 256), device="cuda")
+    out = torch.zeros_like(q)
+    def call(cache=c, q=q, heads=4, out=out, **kw):
+        m.mosaic_cache_attend(cache, q, heads, out, **kw)
+    call()
+    for bad in (dict(heads=3), dict(heads=0), dict(scale=float("nan")), dict(max_len=-1), dict(out=q),
+                dict(scale=3e38)):
+        with pytest.raises(m.MosaicError) as e:
+            call(**bad)
+        assert e.value.status == m.STATUS_INVALID_ARG
+    for bad in (dict(q=q.half()), dict(out=out.bfloat16()), dict(q=q[:, :192]), dict(q=q.cpu()), dict(out=out[:0]),
+                dict(accumulate=True), dict(q=torch.zeros((1, 512), device="cuda")[:, ::2])):
+        with pytest.raises(ValueError):
+            call(**bad)
+    with pytest.raises(m.MosaicError):                      # a row that is not 16-byte aligned
+        call(q=torch.zeros((1, 258), device="cuda")[:, 2:])
+    k = c.k
+    for k2, status in ((torch.zeros((3, 2, 16, 68), dtype=torch.bfloat16, device="cuda"), m.STATUS_UNSUPPORTED),
+                       (torch.zeros((3, 2, 24, 64), dtype=torch.bfloat16, device="cuda"), m.STATUS_UNSUPPORTED),
+                       (torch.zeros((3, 2, 8, 64), dtype=torch.bfloat16, device="cuda"), m.STATUS_UNSUPPORTED),
+                       (torch.zeros((3, 2, 16, 264), dtype=torch.bfloat16, device="cuda"), m.STATUS_UNSUPPORTED),
+                       (torch.zeros((3, 2, 1, 64), dtype=torch.bfloat16, device="cuda").expand(3, 2, 16, 64),
+                        m.STATUS_INVALID_ARG)):
+        with pytest.raises(m.MosaicError) as e:
+            call(cache=m.KVCache(k2, k2, c.block_table, c.state), q=torch.zeros((1, 4 * k2.shape[3]), device="cuda"),
+                 out=torch.zeros((1, 4 * k2.shape[3]), device="cuda"))
+        assert e.value.status == status
+    for cache in (m.KVCache(k, k[:2], c.block_table, c.state), m.KVCache(k, k.float(), c.block_table, c.state),
+                  m.KVCache(k, k, c.block_table.long(), c.state), m.KVCache(k, k, c.block_table, c.state[:1]),
+                  m.KVCache(k.cpu(), k.cpu(), c.block_table, c.state), m.KVCache(k[0], k[0], c.block_table, c.state),
+                  m.KVCache(k.int(), k.int(), c.block_table, c.state)):
+        with pytest.raises(ValueError):
+            call(cache=cache)
