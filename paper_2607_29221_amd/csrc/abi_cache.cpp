@@ -35,7 +35,7 @@ mosaic_status view_of(const mosaic_kv_cache* c, CacheView* v) {
   // the stride of a dimension of one has no meaning
   const int64_t page_stride = c->pages > 1 ? c->page_stride : 0, head_stride = c->kv_heads > 1 ? c->head_stride : 0;
   if (page_stride < 0 || head_stride < 0 || c->token_stride < 0) return fail(MOSAIC_ERR_INVALID_ARG, "negative stride");
-  if (head_stride > INT32_MAX / 4096 || c->token_stride > INT32_MAX / 16384 ||
+  if (head_stride > INT32_MAX / 4096 || c->token_stride > (1 << 27) / c->page_size ||   // a page within 2^30 bytes
       page_stride > INT64_MAX / 8 / (c->pages > 0 ? c->pages : 1))
     return fail(MOSAIC_ERR_UNSUPPORTED, "stride too large");
   if (page_stride * es % 16 != 0 || head_stride * es % 16 != 0 || c->token_stride * es % 16 != 0)
