@@ -11,9 +11,11 @@
 // the launches.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/mosaic.h"
+#include "../../include/mosaic_cache.h"
 #include "dispatch.h"
 
 namespace {
@@ -32,9 +34,15 @@ struct Abi {
   decltype(&mosaic_sparse_gather_cols) gather_cols;
   decltype(&mosaic_hadamard_rotate) hadamard_rotate;
   decltype(&mosaic_quantize_rows) quantize_rows;
+  decltype(&mosaic_cache_append) cache_append;
+  decltype(&mosaic_cache_attend_workspace) cache_attend_workspace;
+  decltype(&mosaic_cache_attend) cache_attend;
+  decltype(&mosaic_cache_evict_workspace) cache_evict_workspace;
+  decltype(&mosaic_cache_evict) cache_evict;
 } abi;
 
 PyObject *s_buf, *s_col0, *s_row_ptr, *s_col_idx, *s_values, *s_rows, *s_cols;   // interned attribute names
+PyObject *s_k, *s_v, *s_block_table, *s_state, *s_weights, *s_order, *s_table, *s_sections, *s_positions, *s_interleaved;
 PyObject *get_device, *get_stream;                                               // torch._C functions
 PyObject* rng_type;                                                              // the ctypes struct of mosaic_rng
 
@@ -453,6 +461,226 @@ FUNCTION(cols_terms, 8) {
   });
 }
 
+// ---------------------------------------------------------------------------
+// Cached decoding
+
+// An attribute that is a plain tensor of dtype dt and dim dimensions; null
+// otherwise (`none` tells None apart). Its owner keeps the tensor.
+const at::Tensor* attr(PyObject* o, PyObject* name, int64_t dim, bool* none = nullptr) {
+  PyObject* v = PyObject_GetAttr(o, name);
+  if (v == nullptr) {
+    PyErr_Clear();
+    return nullptr;
+  }
+  if (none != nullptr) *none = v == Py_None;
+  const at::Tensor* t = v != Py_None ? plain(v) : nullptr;
+  Py_DECREF(v);
+  return t != nullptr && t->dim() == dim ? t : nullptr;
+}
+
+int32_t ftype(at::ScalarType t) {
+  return t == at::kFloat ? MOSAIC_F32 : t == at::kBFloat16 ? MOSAIC_BF16 : t == at::kHalf ? MOSAIC_F16 : -1;
+}
+
+struct Cache {
+  mosaic_kv_cache c;
+  at::ScalarType dtype;
+  at::Device device = at::kCPU;
+  int64_t slots;
+  int32_t* state;
+
+  // weights and order: the cache's or, by `like`, an argument's
+  bool numbers(const at::Tensor* t, at::ScalarType dt) const {
+    return t->scalar_type() == dt && t->dim() == 3 && t->size(0) == c.pages && t->size(1) == c.kv_heads &&
+           t->size(2) == c.page_size && t->is_contiguous() && t->data_ptr() != nullptr;
+  }
+  bool state_like(const at::Tensor* t) const {
+    return t->scalar_type() == at::kInt && t->dim() == 2 && t->size(0) == 2 && t->size(1) == c.batch && t->is_contiguous();
+  }
+  bool get(PyObject* o) {
+    const at::Tensor *k = attr(o, s_k, 4), *v = attr(o, s_v, 4), *t = attr(o, s_block_table, 2), *st = attr(o, s_state, 2);
+    bool no_weights = false, no_order = false;
+    const at::Tensor *w = attr(o, s_weights, 3, &no_weights), *r = attr(o, s_order, 3, &no_order);
+    if (k == nullptr || v == nullptr || t == nullptr || st == nullptr) return false;
+    if ((w == nullptr && !no_weights) || (r == nullptr && !no_order)) return false;
+    c = mosaic_kv_cache{};
+    c.dtype = ftype(k->scalar_type());
+    if (c.dtype < 0 || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes() || v->strides() != k->strides() ||
+        k->stride(3) != 1 || k->numel() == 0)
+      return false;
+    if (t->scalar_type() != at::kInt || t->numel() == 0 || (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    for (int i = 1; i < 4; ++i)
+      if (k->size(i) > INT32_MAX) return false;
+    if (t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) return false;
+    c.batch = (int32_t)t->size(0);
+    c.max_blocks = (int32_t)t->size(1);
+    c.pages = k->size(0);
+    c.kv_heads = (int32_t)k->size(1);
+    c.page_size = (int32_t)k->size(2);
+    c.head_dim = (int32_t)k->size(3);
+    c.page_stride = k->stride(0);
+    c.head_stride = k->stride(1);
+    c.token_stride = k->stride(2);
+    c.ldt = t->stride(0) > t->size(1) ? t->stride(0) : t->size(1);
+    if (!state_like(st) || (w != nullptr && !numbers(w, at::kFloat)) || (r != nullptr && !numbers(r, at::kInt))) return false;
+    c.k = k->data_ptr();
+    c.v = v->data_ptr();
+    c.block_table = (const int32_t*)t->data_ptr();
+    c.weights = w != nullptr ? (float*)w->data_ptr() : nullptr;
+    c.order = r != nullptr ? (int32_t*)r->data_ptr() : nullptr;
+    state = (int32_t*)st->data_ptr();
+    dtype = k->scalar_type();
+    device = k->device();
+    slots = (int64_t)c.max_blocks * c.page_size;
+    return c.k != nullptr && c.v != nullptr && c.block_table != nullptr && state != nullptr;
+  }
+  // rows x cols activations: float32 or of the cache's type
+  bool rows(PyObject* o, int64_t n, int64_t cols, int32_t* type, Mat* m) const {
+    const at::Tensor* t = plain(o);
+    if (t == nullptr || (t->scalar_type() != at::kFloat && t->scalar_type() != dtype)) return false;
+    *type = ftype(t->scalar_type());
+    return matrix(o, n, cols, t->scalar_type(), false, m);
+  }
+  bool new_state(PyObject* o, int32_t** p) const {
+    *p = state;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o);
+    if (t == nullptr || !state_like(t)) return false;
+    *p = (int32_t*)t->data_ptr();
+    return *p != nullptr;
+  }
+};
+
+bool heads_of(PyObject* o, int64_t* heads) { return size(o, heads) && *heads <= INT32_MAX; }
+
+// (cache, qkv, heads, q_out, starts, rotary, new_state)
+FUNCTION(cache_append, 7) {
+  Cache cache;
+  int64_t heads;
+  int32_t xt, qt;
+  Mat x, q, starts;
+  int32_t* new_state;
+  void* s;
+  NEED(cache.get(a[0]) && heads_of(a[2], &heads));
+  const at::Tensor* xten = plain(a[1]);
+  NEED(xten != nullptr && xten->dim() == 2 && xten->size(0) > 0);
+  const int64_t rows = xten->size(0), D = cache.c.head_dim;
+  NEED(cache.rows(a[1], rows, (heads + 2 * (int64_t)cache.c.kv_heads) * D, &xt, &x) &&
+       cache.rows(a[3], rows, heads * D, &qt, &q) && xt == qt);
+  if (a[4] != Py_None) {
+    const at::Tensor* t = plain(a[4]);
+    NEED(t != nullptr && t->dim() == 1 && t->size(0) == cache.c.batch + 1 && vec(a[4], cache.c.batch + 1, at::kInt, false, &starts));
+  }
+  mosaic_rotary r{};
+  if (a[5] != Py_None) {
+    bool none = false;
+    const at::Tensor *table = attr(a[5], s_table, 2), *positions = attr(a[5], s_positions, 2, &none);
+    NEED(table != nullptr && table->scalar_type() == at::kFloat && table->is_contiguous() && table->size(0) > 0);
+    NEED(positions != nullptr || none);
+    PyObject* sections = PyObject_GetAttr(a[5], s_sections);
+    int64_t pairs = 0;
+    bool ok = sections != nullptr && (PyList_CheckExact(sections) || PyTuple_CheckExact(sections));
+    const Py_ssize_t axes = ok ? PySequence_Fast_GET_SIZE(sections) : 0;
+    ok = ok && axes >= 1 && axes <= 4;
+    for (Py_ssize_t i = 0; ok && i < axes; ++i) {
+      int64_t n;
+      ok = integer(PySequence_Fast_GET_ITEM(sections, i), &n) && n >= 0 && n <= D;
+      if (ok) r.sections[i] = (int32_t)n;
+      pairs += ok ? n : 0;
+    }
+    Py_XDECREF(sections);
+    PyErr_Clear();
+    NEED(ok && table->size(1) == 2 * pairs);
+    PyObject* flag = PyObject_GetAttr(a[5], s_interleaved);
+    ok = flag != nullptr && truth(flag, &r.interleaved);
+    Py_XDECREF(flag);
+    PyErr_Clear();
+    NEED(ok);
+    if (positions != nullptr) {
+      NEED(positions->scalar_type() == at::kInt && positions->size(0) >= axes && positions->size(1) >= rows &&
+           positions->stride(1) == 1);
+      r.positions = (const int32_t*)positions->data_ptr();
+      r.ldp = positions->stride(0) > rows ? positions->stride(0) : rows;
+    }
+    r.table = (const float*)table->data_ptr();
+    r.rows = table->size(0);
+    r.naxes = (int32_t)axes;
+  }
+  NEED(cache.new_state(a[6], &new_state) && current_stream(&s));
+  return status([&] {
+    return abi.cache_append(&cache.c, x.p, x.ld, xt, rows, (const int32_t*)starts.p, (int32_t)heads,
+                            a[5] != Py_None ? &r : nullptr, q.p, q.ld, cache.state, new_state, s);
+  });
+}
+
+// The rest of a call that needs `bytes` of memory of its own on the current stream.
+template <class Call>
+PyObject* with_workspace(const at::Device& device, int64_t bytes, Call call) {
+  const at::Tensor work = bytes > 0 ? at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(device)) : at::Tensor();
+  void* p = bytes > 0 ? work.data_ptr() : nullptr;
+  return status([&] { return call(p); });
+}
+
+// (cache, q, heads, out, max_len, scale, accumulate)
+FUNCTION(cache_attend, 7) {
+  Cache cache;
+  int64_t heads, max_len, bytes = 0;
+  int32_t xt, ot, accumulate;
+  Mat q, out;
+  void* s;
+  NEED(cache.get(a[0]) && heads_of(a[2], &heads));
+  const int64_t width = heads * cache.c.head_dim;
+  NEED(cache.rows(a[1], cache.c.batch, width, &xt, &q) && cache.rows(a[3], cache.c.batch, width, &ot, &out) && xt == ot);
+  max_len = cache.slots;
+  NEED(a[4] == Py_None || integer(a[4], &max_len));
+  double scale = 1.0 / sqrt((double)cache.c.head_dim);
+  if (a[5] != Py_None) {
+    NEED(PyFloat_CheckExact(a[5]));
+    scale = PyFloat_AS_DOUBLE(a[5]);
+  }
+  NEED(truth(a[6], &accumulate) && (accumulate == 0 || cache.c.weights != nullptr) && current_stream(&s));
+  // a call that is refused here is refused, with its message, by the Python code
+  NEED(abi.cache_attend_workspace(&cache.c, (int32_t)heads, max_len, accumulate, &bytes) == MOSAIC_OK);
+  return with_workspace(cache.device, bytes, [&](void* work) {
+    return abi.cache_attend(&cache.c, q.p, q.ld, xt, (int32_t)heads, cache.state, max_len, (float)scale, accumulate, out.p,
+                            out.ld, work, bytes, s);
+  });
+}
+
+// (cache, budget, recent, max_len, new_state, new_weights, new_order, kept)
+FUNCTION(cache_evict, 8) {
+  Cache cache;
+  int64_t budget, recent, max_len, bytes = 0;
+  int32_t* new_state;
+  void* s;
+  NEED(cache.get(a[0]) && size(a[1], &budget) && integer(a[2], &recent));
+  NEED(cache.c.weights != nullptr && cache.c.order != nullptr);
+  max_len = cache.slots;
+  NEED((a[3] == Py_None || integer(a[3], &max_len)) && cache.new_state(a[4], &new_state));
+  float* weights = cache.c.weights;
+  int32_t *order = cache.c.order, *kept = nullptr;
+  if (a[5] != Py_None) {
+    const at::Tensor* t = plain(a[5]);
+    NEED(t != nullptr && cache.numbers(t, at::kFloat));
+    weights = (float*)t->data_ptr();
+  }
+  if (a[6] != Py_None) {
+    const at::Tensor* t = plain(a[6]);
+    NEED(t != nullptr && cache.numbers(t, at::kInt));
+    order = (int32_t*)t->data_ptr();
+  }
+  if (a[7] != Py_None) {
+    const at::Tensor* t = plain(a[7]);
+    NEED(t != nullptr && t->scalar_type() == at::kInt && t->dim() == 3 && t->size(0) == cache.c.batch &&
+         t->size(1) == cache.c.kv_heads && t->size(2) == budget && t->is_contiguous() && t->data_ptr() != nullptr);
+    kept = (int32_t*)t->data_ptr();
+  }
+  NEED(current_stream(&s) && abi.cache_evict_workspace(&cache.c, max_len, budget, &bytes) == MOSAIC_OK);
+  return with_workspace(cache.device, bytes, [&](void* work) {
+    return abi.cache_evict(&cache.c, cache.state, new_state, max_len, budget, recent, weights, order, kept, work, bytes, s);
+  });
+}
+
 // bind(addresses, get_device, get_stream, rng_type): addresses of the library's
 // entry points in the order of Abi; torch._C's current device and raw stream;
 // the type that generators are of.
@@ -484,7 +712,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(sample), METHOD(mask), METHOD(masked_matmul), METHOD(integrity_check),
                          METHOD(unmask), METHOD(unmask_words), METHOD(rotate_quantize_mask), METHOD(hadamard_rotate),
-                         METHOD(quantize_rows), METHOD(stream_terms), METHOD(cols_terms), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(quantize_rows), METHOD(stream_terms), METHOD(cols_terms), METHOD(cache_append),
+                         METHOD(cache_attend), METHOD(cache_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -497,6 +726,10 @@ PyMODINIT_FUNC PyInit__binding(void) {
   s_values = PyUnicode_InternFromString("values");
   s_rows = PyUnicode_InternFromString("rows");
   s_cols = PyUnicode_InternFromString("cols");
+  PyObject** const names[] = {&s_k, &s_v, &s_block_table, &s_state, &s_weights, &s_order, &s_table, &s_sections, &s_positions, &s_interleaved};
+  const char* const texts[] = {"k", "v", "block_table", "state", "weights", "order", "table", "sections", "positions", "interleaved"};
+  for (int i = 0; i < 10; ++i)
+    if ((*names[i] = PyUnicode_InternFromString(texts[i])) == nullptr) return nullptr;
   if (!s_buf || !s_col0 || !s_row_ptr || !s_col_idx || !s_values || !s_rows || !s_cols) return nullptr;
   return PyModule_Create(&module);
 }

@@ -100,6 +100,15 @@ __device__ __forceinline__ int32_t page_of(const CacheView& c, int64_t b, int64_
   return p >= 0 && p < c.pages ? p : -1;
 }
 
+// The same for a slot that the whole wave asks for: through the scalar cache
+// (the table is not written while a kernel reads it), so the answer does not
+// wait for the vector loads that are under way.
+typedef const __attribute__((address_space(4))) int32_t* uniform_i32;
+__device__ __forceinline__ int32_t page_of_uniform(const CacheView& c, int64_t b, int32_t slot) {
+  const int32_t p = ((uniform_i32)(uintptr_t)c.table)[b * c.ldt + (slot >> c.log2_page)];
+  return p >= 0 && p < c.pages ? p : -1;
+}
+
 // Bytes from the start of k or v to the row of a head at a place of a page.
 __device__ __forceinline__ int64_t row_offset(const CacheView& c, int32_t page, int32_t head, int64_t slot) {
   return page * c.page_stride + head * c.head_stride + (slot & ((1 << c.log2_page) - 1)) * c.token_stride;

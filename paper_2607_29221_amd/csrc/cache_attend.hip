@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   auto block_at = [&](int slot) {
     Block k = {0, 0};
     if (slot < t1) {
-      const int page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, slot));
+      const int page = page_of_uniform(a.c, b, slot);
       if (page >= 0) {
         k.base = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (slot & page_mask) * ts;
         k.valid = min(t1 - slot, 16);
@@ -413,60 +413,79 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   }
 }
 
-// Joins the pieces of the heads of one key/value head, kJoinHeads at a time,
-// and adds their weights up for a range of tokens (the first range also
-// writes the outputs).
+// Base and sum of a head over its pieces, by one wave.
+__device__ __forceinline__ void head_norm(const float* st, int pieces, int lane, float* common, float* sum) {
+  float m = -INFINITY, l = 0.0f;
+  for (int s = lane; s < pieces; s += 64) m = fmaxf(m, st[2 * s]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  for (int s = lane; s < pieces; s += 64) l += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - m));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+  *common = m == -INFINITY ? 0.0f : m;
+  *sum = l;
+}
+
+// Joins the pieces. The first `group` workgroups of a key/value head write one
+// query head's output each: rows of 16-byte columns, the pieces dealt out to
+// the rows of threads. The others add the weights of kJoinTokens tokens up,
+// over the heads of the group.
 constexpr int kJoinHeads = 16, kJoinTokens = 1024;
 template <int XT>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk) {
   typedef typename FloatType<XT>::type X;
+  __shared__ f32x4 rows[256];
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.y, b = blockIdx.z, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int n = held_tokens(a.lengths, b, a.max_len);
-  const int t0 = blockIdx.x * kJoinTokens;
-  if (t0 > 0 && t0 >= n) return;
   const int pieces = n == 0 ? 1 : (n + wk.piece - 1) / wk.piece;
+  if ((int)blockIdx.x < group) {
+    const int64_t row = (int64_t)b * a.heads + h * group + blockIdx.x;
+    const float* st = wk.stat + 2 * row * wk.pieces;
+    float common, sum;
+    head_norm(st, pieces, lane, &common, &sum);   // every wave for itself
+    const int cols = D / 4, at_once = 256 / cols, c = tid % cols, s0 = tid / cols;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (s0 < at_once) {
+      const float* part = wk.part + row * wk.pieces * D + 4 * c;
+#pragma unroll 4
+      for (int s = s0; s < pieces; s += at_once)
+        o += *(const f32x4*)(part + (int64_t)s * D) * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - common));
+    }
+    rows[tid] = o;
+    __syncthreads();
+    if (tid >= cols) return;
+    for (int s = 1; s < at_once; ++s) o += rows[s * cols + tid];
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + blockIdx.x) * D + 4 * tid;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
+    return;
+  }
+  const int t0 = ((int)blockIdx.x - group) * kJoinTokens;
+  if (t0 >= n) return;
   float w[kJoinTokens / 256] = {};
   for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
     const int count = min(group - g0, kJoinHeads);
     const int64_t row0 = (int64_t)b * a.heads + h * group + g0;
     __syncthreads();
     for (int g = wave; g < count; g += 4) {
-      const float* st = wk.stat + 2 * (row0 + g) * wk.pieces;
-      float common = -INFINITY, sum = 0.0f;
-      for (int s = lane; s < pieces; s += 64) common = fmaxf(common, st[2 * s]);
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) common = fmaxf(common, __shfl_xor(common, off));
-      for (int s = lane; s < pieces; s += 64) sum += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - common));
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+      float common, sum;
+      head_norm(wk.stat + 2 * (row0 + g) * wk.pieces, pieces, lane, &common, &sum);
       if (lane == 0) {
-        norm[g][0] = common == -INFINITY ? 0.0f : common;
+        norm[g][0] = common;
         norm[g][1] = sum == 0.0f ? 0.0f : 1.0f / sum;
       }
     }
     __syncthreads();
-    if (t0 == 0) {
-      for (int u = tid; u < count * D; u += 256) {
-        const int g = u / D, d = u - g * D;
-        const float* st = wk.stat + 2 * (row0 + g) * wk.pieces;
-        const float* part = wk.part + (row0 + g) * wk.pieces * D + d;
-        float o = 0.0f;
-        for (int s = 0; s < pieces; ++s) o += part[(int64_t)s * D] * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - norm[g][0]));
-        ((X*)((char*)a.out + (int64_t)b * a.ldo))[(int64_t)(h * group + g0 + g) * D + d] = (X)(o * norm[g][1]);
-      }
-    }
-    if (a.accumulate) {
 #pragma unroll
-      for (int k = 0; k < kJoinTokens / 256; ++k) {
-        const int t = t0 + 256 * k + tid;
-        if (t < n)
-          for (int g = 0; g < count; ++g) w[k] += exp2_fast(wk.scores[(row0 + g) * wk.row + t] - norm[g][0]) * norm[g][1];
-      }
+    for (int k = 0; k < kJoinTokens / 256; ++k) {
+      const int t = t0 + 256 * k + tid;
+      if (t < n)
+        for (int g = 0; g < count; ++g) w[k] += exp2_fast(wk.scores[(row0 + g) * wk.row + t] - norm[g][0]) * norm[g][1];
     }
   }
-  if (!a.accumulate) return;
 #pragma unroll
   for (int k = 0; k < kJoinTokens / 256; ++k) {
     const int t = t0 + 256 * k + tid;
@@ -489,8 +508,8 @@ hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
   else if (a.c.head_dim <= 128) cache_attend_kernel<CT, XT, 128><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
   else cache_attend_kernel<CT, XT, 256><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
   if (p.join) {
-    const unsigned ranges = a.accumulate && a.max_len > 0 ? (unsigned)((a.max_len + kJoinTokens - 1) / kJoinTokens) : 1u;
-    cache_join_kernel<XT><<<dim3(ranges, a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, w);
+    const int64_t ranges = a.accumulate ? (a.max_len + kJoinTokens - 1) / kJoinTokens : 0;
+    cache_join_kernel<XT><<<dim3((unsigned)(a.heads / a.c.kv_heads + ranges), a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, w);
   }
   return hipGetLastError();
 }

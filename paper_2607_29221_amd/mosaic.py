@@ -43,7 +43,9 @@ def _check(status: int, name: str) -> None:
 # Entry points that _binding.so calls, in the order it expects.
 _BOUND = ("mosaic_sample", "mosaic_mask", "mosaic_masked_matmul", "mosaic_integrity_check", "mosaic_unmask",
           "mosaic_unmask_words", "mosaic_rotate_quantize_mask", "mosaic_sparse_stream_gather_rows_terms",
-          "mosaic_sparse_gather_cols_terms", "mosaic_sparse_gather_cols", "mosaic_hadamard_rotate", "mosaic_quantize_rows")
+          "mosaic_sparse_gather_cols_terms", "mosaic_sparse_gather_cols", "mosaic_hadamard_rotate", "mosaic_quantize_rows",
+          "mosaic_cache_append", "mosaic_cache_attend_workspace", "mosaic_cache_attend",
+          "mosaic_cache_evict_workspace", "mosaic_cache_evict")
 _b = None
 
 
@@ -644,6 +646,9 @@ def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: to
     kv_heads heads): rotated queries to q_out, rotated keys and values into
     the cache. Rows starts[b] .. starts[b + 1] - 1 are sequence b's (None: row
     b). The state is advanced in place unless new_state is given."""
+    st = (_b or _native()).cache_append(cache, qkv, heads, q_out, starts, rotary, new_state)
+    if st is not None:
+        return _check(st, "mosaic_cache_append")
     c = _cache_arg(cache)
     rows = qkv.shape[0]
     _cache_rows(qkv, rows, (heads + 2 * c.kv_heads) * c.head_dim, "qkv", cache)
@@ -685,6 +690,9 @@ def mosaic_cache_attend(cache: KVCache, q: torch.Tensor, heads: int, out: torch.
     tokens that sequence b holds; ``accumulate`` adds the attention weights
     up in cache.weights. ``max_len``: no sequence holds more tokens (None: as
     many as there are slots). ``scale`` defaults to 1 / sqrt(head_dim)."""
+    st = (_b or _native()).cache_attend(cache, q, heads, out, max_len, scale, accumulate)
+    if st is not None:
+        return _check(st, "mosaic_cache_attend")
     c = _cache_arg(cache)
     _cache_rows(q, c.batch, heads * c.head_dim, "q", cache)
     _cache_rows(out, c.batch, heads * c.head_dim, "out", cache)
@@ -710,6 +718,9 @@ def mosaic_cache_evict(cache: KVCache, budget: int, recent: int, max_len: Option
     weights, moved into its first ``budget`` slots. Weights, order and state
     change in place unless others are given; ``kept`` (int32, batch x kv_heads
     x budget) gets the slot that each slot's token had before."""
+    st = (_b or _native()).cache_evict(cache, budget, recent, max_len, new_state, new_weights, new_order, kept)
+    if st is not None:
+        return _check(st, "mosaic_cache_evict")
     c = _cache_arg(cache)
     if cache.weights is None or cache.order is None:
         raise ValueError("eviction needs a cache with weights and order")
