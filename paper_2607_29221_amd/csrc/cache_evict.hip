@@ -1,21 +1,28 @@
 // Eviction by accumulated weight (mosaic_cache_evict).
 //
-// One workgroup selects for one key/value head of one sequence: the rank of a
-// token is a 32-bit key, the budget-th largest key is found digit by digit
-// (counts of the digits' values in LDS, integers, so no order of the atomics
-// shows), and a scan over the slots in their order numbers the survivors,
-// which settles ties and pairs the r-th survivor beyond the budget with the
-// r-th slot that came free below it. A second kernel copies rows along these
-// pairs: sources lie at or beyond the budget and destinations below it, so
-// the copies are independent.
+// The rank of a token is a 32-bit key, and the budget-th largest key of a
+// key/value head is found digit by digit (11, 11 and 10 bits): counts of a
+// digit's values in LDS, integers, so no order of the atomics shows. Counting
+// the survivors over the slots in their order then settles ties and numbers
+// both sides of the move: the r-th slot that came free below the budget takes
+// the r-th survivor from beyond it. Sources lie at or beyond the budget and
+// destinations below it, so a last kernel copies rows along these pairs in any
+// order.
+//
+// Up to kShortSlots slots one workgroup takes a head: its keys stay in
+// registers through all the steps. Beyond, a workgroup takes kChunk slots and
+// the steps are launches: counts of the first, second and third digit (each
+// finds the digit before it from the counts of all chunks), then the numbering.
 #include "cache.h"
 #include "dispatch.h"
 
 namespace mosaic {
 namespace {
 
-constexpr int kSelectThreads = 1024;
-constexpr int kWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+constexpr int kShortSlots = 8192;
+constexpr int kChunk = 8192, kChunkThreads = 1024, kChunkKeys = kChunk / kChunkThreads;
+constexpr int kFew = 4;                   // evictions that are found one by one
 
 // Rank of a token; a larger key stays before a smaller one. The latest come
 // first, then weights as numbers (0 and -0 alike), then NaN, then slots whose
@@ -28,145 +35,439 @@ __device__ __forceinline__ uint32_t rank_key(float w, bool latest) {
   return (u >> 31) != 0u ? ~u : u | 0x80000000u;
 }
 
-// Lists of one (sequence, head): keys by slot, then pairs of slots.
+// Of one (sequence, head): the slots that came free below the budget, in
+// order; the survivors beyond it, from the last to the first; how many.
+// Beyond kShortSlots also keys by slot, the counts of the three digits by
+// chunk, the digits found so far with the number still needed below them, and
+// the survivors of each chunk that are above the digits found so far.
 struct Lists {
-  uint32_t* keys;
-  int32_t* holes;
-  int32_t* movers;
-  int32_t* count;
+  int32_t *free_slots, *movers, *count;
+  uint32_t *keys, *counts[3], *found, *above;
+  int64_t chunks;
 };
 int64_t most_moves(int64_t max_len, int64_t budget) {
   const int64_t beyond = max_len - budget;
   return beyond <= 0 ? 0 : beyond < budget ? beyond : budget;
 }
-__device__ __forceinline__ Lists lists_of(const EvictLaunch& a, int64_t moves, int64_t bh, int64_t all) {
-  uint32_t* keys = (uint32_t*)a.workspace;
-  int32_t* holes = (int32_t*)(keys + all * a.max_len);
-  int32_t* movers = holes + all * moves;
-  return {keys + bh * a.max_len, holes + bh * moves, movers + bh * moves, movers + all * moves + bh};
+__host__ __device__ inline int64_t chunks_of(int64_t max_len) {
+  return max_len <= kShortSlots ? 0 : (max_len + kChunk - 1) / kChunk;
+}
+// words of the workspace per (sequence, head)
+int64_t list_words(int64_t max_len, int64_t budget) {
+  const int64_t moves = most_moves(max_len, budget), chunks = chunks_of(max_len);
+  return moves == 0 ? 0 : 2 * moves + 1 + (chunks > 0 ? max_len + 3 * kBins * chunks + 4 + chunks : 0);
+}
+__device__ __forceinline__ Lists lists_of(const EvictLaunch& a, int64_t moves, int64_t bh) {
+  const int64_t all = (int64_t)a.c.batch * a.c.kv_heads;
+  Lists l;
+  l.chunks = chunks_of(a.max_len);
+  uint32_t* p = (uint32_t*)a.workspace;
+  for (int d = 0; d < 3; ++d) {
+    l.counts[d] = p + bh * l.chunks * kBins;
+    p += all * l.chunks * kBins;
+  }
+  if (l.chunks > 0) {
+    l.found = p + 4 * bh;
+    l.above = p + 4 * all + bh * l.chunks;
+    l.keys = p + (4 + l.chunks) * all + bh * a.max_len;
+    p += all * (4 + l.chunks + a.max_len);
+  }
+  l.free_slots = (int32_t*)p + bh * moves;
+  l.movers = (int32_t*)p + (all + bh) * moves;
+  l.count = (int32_t*)p + 2 * all * moves + bh;
+  return l;
 }
 
-__device__ __forceinline__ void copy_numbers(const EvictLaunch& a, int64_t from, int64_t to) {
-  a.new_weights[to] = a.c.weights[from];
-  a.new_order[to] = a.c.order[from];
+// Digit d of the key: its lowest bit and its width.
+__device__ __forceinline__ int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int d) {
+  return (key >> digit_shift(d)) & (d == 2 ? 1023u : 2047u);
+}
+// whether a key agrees with the digits before d
+__device__ __forceinline__ bool agrees(uint32_t key, uint32_t prefix, int d) {
+  return d == 0 || (key >> digit_shift(d - 1)) == prefix;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictLaunch a, int64_t moves) {
-  __shared__ uint32_t bins[2048];
-  __shared__ uint32_t part[2 * kWaves];
-  __shared__ uint32_t found[2];
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t bh = (int64_t)b * a.c.kv_heads + h, all = (int64_t)a.c.batch * a.c.kv_heads;
-  const Lists l = lists_of(a, moves, bh, all);
-  const int32_t n = held_tokens(a.state, b, a.max_len);
-  const int64_t latest = (int64_t)a.state[a.c.batch + b] - a.recent;
-  int32_t* kept = a.kept != nullptr ? a.kept + bh * a.budget : nullptr;
-  const bool apart = a.new_weights != a.c.weights || a.new_order != a.c.order;
-
-  if (n <= a.budget) {
-    for (int64_t i = tid; i < n; i += kSelectThreads) {
-      const int32_t page = page_of(a.c, b, i);
-      if (apart && page >= 0) copy_numbers(a, row_index(a.c, page, h, i), row_index(a.c, page, h, i));
+// From counts of a digit (thread t holds those of values kBins - 1 - PER t
+// downwards in own[0 ..]): the value at which the running sum from the top
+// reaches `need`, and what is still needed within it. All threads.
+template <int THREADS>
+__device__ __forceinline__ void find_digit(const uint32_t (&own)[kBins / THREADS], uint32_t need, uint32_t* part,
+                                           uint32_t* found) {
+  constexpr int PER = kBins / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t total = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) total += own[k];
+  uint32_t sum = total;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(sum, off);
+    if (lane >= off) sum += o;
+  }
+  if (lane == 63) part[wave] = sum;
+  __syncthreads();
+  uint32_t before = sum - total;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) before += w < wave ? part[w] : 0u;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (before < need && before + own[k] >= need) {
+      found[0] = (uint32_t)(kBins - 1 - PER * tid - k);
+      found[1] = need - before;
     }
-    if (kept != nullptr)
-      for (int64_t i = tid; i < a.budget; i += kSelectThreads) kept[i] = i < n ? (int32_t)i : -1;
-    if (tid == 0 && moves > 0) *l.count = 0;
+    before += own[k];
+  }
+  __syncthreads();
+}
+
+// The numbers of a token that stays in its slot, to wherever they are wanted.
+__device__ __forceinline__ void stay(const EvictLaunch& a, int32_t* kept, bool apart, int64_t row, int32_t slot,
+                                     float w, int32_t o) {
+  if (apart && row >= 0) {
+    a.new_weights[row] = w;
+    a.new_order[row] = o;
+  }
+  if (kept != nullptr) kept[slot] = slot;
+}
+
+// A workgroup's slots first + THREADS r + tid: keys, and what they come from.
+template <int R> struct Tokens {
+  uint32_t key[R];
+  float w[R];
+  int32_t o[R];
+  int64_t row[R];         // index into weights and order, -1 if there is none
+};
+template <int THREADS, int R>
+__device__ __forceinline__ void load_tokens(const EvictLaunch& a, int b, int h, int32_t first, int32_t n, int64_t latest,
+                                            Tokens<R>& t) {
+  const float* weights = a.c.pages > 0 ? a.c.weights : (const float*)a.state;
+  const int32_t* order = a.c.pages > 0 ? a.c.order : a.state;
+  int32_t page[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int32_t i = first + THREADS * r + (int)threadIdx.x;
+    page[r] = page_of(a.c, b, min(i, n - 1));
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int32_t i = min(first + THREADS * r + (int)threadIdx.x, n - 1);
+    t.row[r] = page[r] >= 0 ? row_index(a.c, page[r], h, i) : -1;
+    const int64_t safe = page[r] >= 0 ? t.row[r] : 0;     // a load that every lane can make
+    t.w[r] = weights[safe];
+    t.o[r] = order[safe];
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) t.key[r] = t.row[r] >= 0 ? rank_key(t.w[r], t.o[r] >= latest) : kAbsent;
+}
+
+// Numbers the slots first .. of a workgroup, of which `above` lower ones have
+// a key over `least` and `equal` a key like it (of those `need` stay), and
+// writes the lists. cnt: THREADS / 64 * R words.
+template <int THREADS, int R, bool LOADED>
+__device__ __forceinline__ void number_slots(const EvictLaunch& a, int b, int h, const Lists& l, int32_t* kept, bool apart,
+                                             int32_t first, int32_t n, uint32_t least, uint32_t need, uint32_t above,
+                                             uint32_t equal, const Tokens<R>& t, uint32_t* cnt) {
+  constexpr int NW = THREADS / 64, ENTRIES = NW * R, EACH = (ENTRIES + 63) / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t budget = (int32_t)a.budget;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool in = first + THREADS * r + tid < n;
+    const uint32_t g = (uint32_t)__popcll(__ballot(in && t.key[r] > least)), e = (uint32_t)__popcll(__ballot(in && t.key[r] == least));
+    if (lane == 0) cnt[NW * r + wave] = g << 16 | e;        // at most kShortSlots of each
+  }
+  __syncthreads();
+  if (wave == 0) {
+    uint32_t v[EACH], sum = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int at = EACH * lane + k;
+      v[k] = at < ENTRIES ? cnt[at] : 0u;
+      sum += v[k];
+    }
+    uint32_t run = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t o = __shfl_up(run, off);
+      if (lane >= off) run += o;
+    }
+    run -= sum;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      if (EACH * lane + k < ENTRIES) cnt[EACH * lane + k] = run;
+      run += v[k];
+    }
+  }
+  __syncthreads();
+  const uint64_t under = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int32_t i = first + THREADS * r + tid;
+    const bool in = i < n, gt = in && t.key[r] > least, eq = in && t.key[r] == least;
+    const uint64_t mg = __ballot(gt), me = __ballot(eq);
+    const uint32_t base = cnt[NW * r + wave];
+    const uint32_t g = above + (base >> 16) + (uint32_t)__popcll(mg & under);
+    const uint32_t e = equal + (base & 0xFFFFu) + (uint32_t)__popcll(me & under);
+    const int32_t rank = (int32_t)(g + (e < need ? e : need));    // survivors in lower slots
+    const bool stays = gt || (eq && e < need);
+    if (i == budget) *l.count = budget - rank;
+    if (i < budget && in) {
+      if (!stays) {
+        l.free_slots[i - rank] = i;
+      } else if (LOADED) {
+        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
+      } else {
+        const int32_t page = apart ? page_of(a.c, b, i) : -1;
+        const int64_t row = page >= 0 ? row_index(a.c, page, h, i) : -1;
+        stay(a, kept, apart, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
+      }
+    } else if (stays) {
+      l.movers[budget - 1 - rank] = i;
+    }
+  }
+}
+
+__device__ __forceinline__ int64_t first_latest(const EvictLaunch& a, int b) {
+  return (int64_t)a.state[a.c.batch + b] - a.recent;
+}
+__device__ __forceinline__ bool apart_of(const EvictLaunch& a) {
+  return a.new_weights != a.c.weights || a.new_order != a.c.order;
+}
+
+// One head, all its keys in registers.
+template <int THREADS, int R>
+__global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, int64_t moves) {
+  constexpr int NW = THREADS / 64, PER = kBins / THREADS;
+  __shared__ uint32_t bins[kBins];
+  __shared__ uint32_t part[NW], found[2], cnt[NW * R];
+  __shared__ uint64_t worst[NW];
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t bh = (int64_t)b * a.c.kv_heads + h;
+  const int32_t n = held_tokens(a.state, b, a.max_len);
+  int32_t* kept = a.kept != nullptr ? a.kept + bh * a.budget : nullptr;
+  const bool apart = apart_of(a);
+  const Lists l = lists_of(a, moves, bh);
+  if (n <= a.budget && moves > 0 && tid == 0) *l.count = 0;
+  if (kept != nullptr)
+    for (int64_t i = n + tid; i < a.budget; i += THREADS) kept[i] = -1;
+  if (n == 0) return;
+  Tokens<R> t;
+  load_tokens<THREADS, R>(a, b, h, 0, n, first_latest(a, b), t);
+  if (n <= a.budget) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (THREADS * r + tid < n) stay(a, kept, apart, t.row[r], THREADS * r + tid, t.w[r], t.o[r]);
     return;
   }
   const int32_t budget = (int32_t)a.budget;
 
-  // the budget-th largest key, from its upper digits to its lower ones
-  uint32_t prefix = 0, need = (uint32_t)budget;
-  for (int shift = 21, bits = 11; ; shift -= bits) {
-    const int width = shift == 0 ? 10 : 11;
-    for (int i = tid; i < 2048; i += kSelectThreads) bins[i] = 0u;
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelectThreads) {
-      uint32_t key;
-      if (shift == 21) {
-        const int32_t page = page_of(a.c, b, i);
-        key = kAbsent;
-        if (page >= 0) {
-          const int64_t r = row_index(a.c, page, h, i);
-          key = rank_key(a.c.weights[r], a.c.order[r] >= latest);
-        }
-        l.keys[i] = key;
-      } else {
-        key = l.keys[i];
+  if (n - budget <= kFew) {
+    // a step of a loop at its budget: the smallest key goes, of equal ones the
+    // last, once or a few times
+    uint32_t gone = 0;                            // of this thread's slots, by bits
+    int32_t out[kFew];
+    const int32_t evicted = n - budget;
+#pragma unroll
+    for (int k = 0; k < kFew; ++k) {
+      if (k >= evicted) break;
+      uint64_t m = ~(uint64_t)0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int32_t i = THREADS * r + tid;
+        const uint64_t v = (uint64_t)t.key[r] << 32 | (uint32_t)~i;
+        if (i < n && ((gone >> r) & 1u) == 0u && v < m) m = v;
       }
-      if (shift == 21 || (key >> (shift + width)) == prefix) atomicAdd(&bins[(key >> shift) & ((1u << width) - 1)], 1u);
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) {
+        const uint64_t o = __shfl_xor(m, off);
+        m = o < m ? o : m;
+      }
+      if (lane == 0) worst[wave] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m = worst[w] < m ? worst[w] : m;
+      __syncthreads();
+      out[k] = (int32_t)~(uint32_t)m;
+      if (out[k] % THREADS == tid) gone |= 1u << (out[k] / THREADS);
     }
-    __syncthreads();
-    // thread t holds bins 2047 - 2t and 2046 - 2t: sums from the top
-    const uint32_t hi = bins[2047 - 2 * tid], lo = bins[2046 - 2 * tid];
-    uint32_t sum = hi + lo;
-    for (int off = 1; off < 64; off <<= 1) {
-      const uint32_t o = __shfl_up(sum, off);
-      if (lane >= off) sum += o;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int32_t i = THREADS * r + tid;
+      if (i >= n) continue;
+      const bool stays = ((gone >> r) & 1u) == 0u;
+      if (i < budget && stays) {
+        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
+      } else if (i < budget || stays) {
+        int32_t lower = 0, lower_within = 0;      // evicted slots below i, and those within the budget
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) {
+          lower += k < evicted && out[k] < i ? 1 : 0;
+          lower_within += k < evicted && out[k] < budget ? 1 : 0;
+        }
+        if (i < budget) l.free_slots[lower] = i;
+        else l.movers[lower_within - 1 - (i - budget - (lower - lower_within))] = i;
+      }
+      if (i == budget) {
+        int32_t count = 0;
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) count += k < evicted && out[k] < budget ? 1 : 0;
+        *l.count = count;
+      }
     }
-    if (lane == 63) part[wave] = sum;
+    return;
+  }
+
+  uint32_t prefix = 0, need = (uint32_t)budget;
+#pragma unroll
+  for (int d = 0; d < 3; ++d) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) bins[THREADS * k + tid] = 0u;
     __syncthreads();
-    uint32_t before = sum - hi - lo;
-    for (int w = 0; w < wave; ++w) before += part[w];
-    if (before < need && before + hi + lo >= need) {
-      const bool upper = before + hi >= need;
-      found[0] = upper ? 2047 - 2 * tid : 2046 - 2 * tid;
-      found[1] = need - before - (upper ? 0u : hi);
-    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (THREADS * r + tid < n && agrees(t.key[r], prefix, d)) atomicAdd(&bins[digit_of(t.key[r], d)], 1u);
     __syncthreads();
-    prefix = (prefix << width) | found[0];
+    uint32_t own[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) own[k] = bins[kBins - 1 - PER * tid - k];
+    find_digit<THREADS>(own, need, part, found);
+    prefix = prefix << (d == 2 ? 10 : 11) | found[0];
     need = found[1];
     __syncthreads();
-    if (shift == 0) break;
-    bits = shift == 21 ? 11 : 10;
   }
-  const uint32_t least = prefix;                 // keys above stay, and the first `need` equal to it
+  number_slots<THREADS, R, true>(a, b, h, l, kept, apart, 0, n, prefix, need, 0u, 0u, t, cnt);
+}
 
-  uint32_t above = 0, equal = 0;                 // in the slots before this round's
-  int32_t kept_low = 0;
-  for (int64_t i0 = 0; i0 < n; i0 += kSelectThreads) {
-    const int64_t i = i0 + tid;
-    const uint32_t key = i < n ? l.keys[i] : 0u;
-    const bool gt = i < n && key > least, eq = i < n && key == least;
-    const uint64_t mg = __ballot(gt), me = __ballot(eq);
-    if (lane == 0) {
-      part[2 * wave] = (uint32_t)__popcll(mg);
-      part[2 * wave + 1] = (uint32_t)__popcll(me);
+// Long sequences: the counts of digit D, in chunks of slots.
+template <int D>
+__global__ __launch_bounds__(kChunkThreads) void cache_count_kernel(EvictLaunch a, int64_t moves) {
+  constexpr int PER = kBins / kChunkThreads;
+  __shared__ uint32_t bins[kBins];
+  __shared__ uint32_t part[kChunkThreads / 64], found[2];
+  const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t bh = (int64_t)b * a.c.kv_heads + h;
+  const int32_t n = held_tokens(a.state, b, a.max_len), first = chunk * kChunk;
+  if (n <= a.budget || first >= n) return;
+  const Lists l = lists_of(a, moves, bh);
+  uint32_t key[kChunkKeys];
+  if (D == 0) {
+    Tokens<kChunkKeys> t;
+    load_tokens<kChunkThreads, kChunkKeys>(a, b, h, first, n, first_latest(a, b), t);
+#pragma unroll
+    for (int r = 0; r < kChunkKeys; ++r) {
+      const int32_t i = first + kChunkThreads * r + tid;
+      key[r] = t.key[r];
+      if (i < n) l.keys[i] = key[r];
     }
-    __syncthreads();
-    const uint64_t under = ((uint64_t)1 << lane) - 1;
-    uint32_t g = above + (uint32_t)__popcll(mg & under), e = equal + (uint32_t)__popcll(me & under);
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) {
-        g += part[2 * w];
-        e += part[2 * w + 1];
-      }
-      above += part[2 * w];
-      equal += part[2 * w + 1];
-    }
-    const bool stays = gt || (eq && e < need);
-    const int32_t rank = (int32_t)(g + (e < need ? e : need));    // survivors in lower slots
-    if (i == budget) found[0] = (uint32_t)rank;
-    __syncthreads();
-    if (i0 + kSelectThreads > budget && i0 <= budget) kept_low = (int32_t)found[0];
-    if (i < budget) {
-      if (!stays) l.holes[i - rank] = (int32_t)i;
-      else {
-        const int32_t page = page_of(a.c, b, i);
-        if (apart && page >= 0) copy_numbers(a, row_index(a.c, page, h, i), row_index(a.c, page, h, i));
-        if (kept != nullptr) kept[i] = (int32_t)i;
-      }
-    } else if (i < n && stays) {
-      l.movers[rank - kept_low] = (int32_t)i;
+  } else {
+#pragma unroll
+    for (int r = 0; r < kChunkKeys; ++r) key[r] = l.keys[min(first + kChunkThreads * r + tid, n - 1)];
+  }
+  uint32_t prefix = 0;
+  if (D > 0) {
+    const int chunks = (n + kChunk - 1) / kChunk;
+    uint32_t own[PER] = {};
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c)
+#pragma unroll
+      for (int k = 0; k < PER; ++k) own[k] += l.counts[D - 1][(int64_t)c * kBins + kBins - 1 - PER * tid - k];
+    const uint32_t before = D > 1 ? l.found[0] : 0u;
+    find_digit<kChunkThreads>(own, D > 1 ? l.found[1] : (uint32_t)a.budget, part, found);
+    prefix = before << 11 | found[0];
+    if (chunk == 0 && tid == 0) {
+      l.found[2 * (D - 1)] = prefix;
+      l.found[2 * (D - 1) + 1] = found[1];
     }
   }
-  if (tid == 0) *l.count = budget - kept_low;
+  if (D == 2) {
+    // this chunk's survivors by the digits found so far
+    uint32_t above = 0;
+#pragma unroll
+    for (int r = 0; r < kChunkKeys; ++r)
+      above += (uint32_t)__popcll(__ballot(first + kChunkThreads * r + tid < n && (key[r] >> digit_shift(D - 1)) > prefix));
+    __syncthreads();
+    if (lane == 0) part[wave] = above;
+    __syncthreads();
+    if (tid == 0) {
+      above = 0;
+      for (int w = 0; w < kChunkThreads / 64; ++w) above += part[w];
+      l.above[chunk] = above;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) bins[kChunkThreads * k + tid] = 0u;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kChunkKeys; ++r)
+    if (first + kChunkThreads * r + tid < n && agrees(key[r], prefix, D)) atomicAdd(&bins[digit_of(key[r], D)], 1u);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k) l.counts[D][(int64_t)chunk * kBins + kChunkThreads * k + tid] = bins[kChunkThreads * k + tid];
+}
+
+__global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch a, int64_t moves) {
+  constexpr int PER = kBins / kChunkThreads, NW = kChunkThreads / 64;
+  __shared__ uint32_t part[NW], found[2], cnt[NW * kChunkKeys], lower[2];
+  const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t bh = (int64_t)b * a.c.kv_heads + h;
+  const int32_t n = held_tokens(a.state, b, a.max_len), first = chunk * kChunk;
+  int32_t* kept = a.kept != nullptr ? a.kept + bh * a.budget : nullptr;
+  const bool apart = apart_of(a);
+  const Lists l = lists_of(a, moves, bh);
+  if (kept != nullptr)
+    for (int64_t i = n + (int64_t)chunk * kChunkThreads + tid; i < a.budget; i += (int64_t)gridDim.x * kChunkThreads) kept[i] = -1;
+  if (n <= a.budget) {
+    if (chunk == 0 && tid == 0 && moves > 0) *l.count = 0;
+    for (int32_t i = first + tid; i < min(n, first + kChunk); i += kChunkThreads) {
+      const int32_t page = page_of(a.c, b, i);
+      const int64_t row = page >= 0 ? row_index(a.c, page, h, i) : -1;
+      stay(a, kept, apart, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
+    }
+    return;
+  }
+  if (first >= n) return;
+  Tokens<kChunkKeys> t;
+#pragma unroll
+  for (int r = 0; r < kChunkKeys; ++r) t.key[r] = l.keys[min(first + kChunkThreads * r + tid, n - 1)];
+  // the last digit, and how many of its values lie in the chunks before
+  const int chunks = (n + kChunk - 1) / kChunk;
+  uint32_t own[PER] = {}, earlier[PER] = {}, above = 0;
+#pragma unroll 8
+  for (int c = 0; c < chunks; ++c)
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint32_t v = l.counts[2][(int64_t)c * kBins + kBins - 1 - PER * tid - k];
+      own[k] += v;
+      earlier[k] += c < chunk ? v : 0u;
+    }
+  for (int c = tid; c < chunk; c += kChunkThreads) above += l.above[c];
+  find_digit<kChunkThreads>(own, l.found[3], part, found);
+  const uint32_t digit = found[0], need = found[1], least = l.found[2] << 10 | digit;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t value = (uint32_t)(kBins - 1 - PER * tid - k);
+    if (value > digit) above += earlier[k];
+    if (value == digit) lower[1] = earlier[k];
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off);
+  __syncthreads();
+  if (lane == 0) part[wave] = above;
+  __syncthreads();
+  if (tid == 0) {
+    above = 0;
+    for (int w = 0; w < NW; ++w) above += part[w];
+    lower[0] = above;
+  }
+  __syncthreads();
+  number_slots<kChunkThreads, kChunkKeys, false>(a, b, h, l, kept, apart, first, n, least, need, lower[0], lower[1], t, cnt);
 }
 
 // Copies rows along the pairs of slots, 16 bytes per thread.
 __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t moves, int32_t per_block) {
   const int h = blockIdx.y, b = blockIdx.z;
-  const int64_t bh = (int64_t)b * a.c.kv_heads + h, all = (int64_t)a.c.batch * a.c.kv_heads;
+  const int64_t bh = (int64_t)b * a.c.kv_heads + h;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
     const int32_t n = held_tokens(a.state, b, a.max_len);
     const int32_t seen = a.state[a.c.batch + b];
@@ -174,14 +475,13 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
     a.new_state[a.c.batch + b] = seen;
   }
   if (moves == 0) return;
-  const Lists l = lists_of(a, moves, bh, all);
-  const int32_t first = (int32_t)blockIdx.x * per_block;
-  int32_t count = *l.count - first;
-  count = count < per_block ? count : per_block;
+  const Lists l = lists_of(a, moves, bh);
+  const int32_t all = *l.count, first = (int32_t)blockIdx.x * per_block;
+  const int32_t count = min(all - first, per_block);
   const int32_t chunks = a.c.head_dim * (a.c.dtype == MOSAIC_F32 ? 4 : 2) / 16;
   for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {
     const int32_t m = w / chunks, c = w - m * chunks;
-    const int32_t from = l.movers[first + m], to = l.holes[first + m];
+    const int32_t from = l.movers[all - 1 - (first + m)], to = l.free_slots[first + m];
     const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);
     if (pf < 0 || pt < 0) continue;
     const int64_t of = row_offset(a.c, pf, h, from) + 16 * c, ot = row_offset(a.c, pt, h, to) + 16 * c;
@@ -189,7 +489,9 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
     *(uint4*)(a.c.k + ot) = k;
     *(uint4*)(a.c.v + ot) = v;
     if (c == 0) {
-      copy_numbers(a, row_index(a.c, pf, h, from), row_index(a.c, pt, h, to));
+      const int64_t rf = row_index(a.c, pf, h, from), rt = row_index(a.c, pt, h, to);
+      a.new_weights[rt] = a.c.weights[rf];
+      a.new_order[rt] = a.c.order[rf];
       if (a.kept != nullptr) a.kept[bh * a.budget + to] = from;
     }
   }
@@ -198,13 +500,27 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
 }  // namespace
 
 int64_t cache_evict_workspace(const CacheView& c, int64_t max_len, int64_t budget) {
-  const int64_t moves = most_moves(max_len, budget);
-  return moves == 0 ? 0 : (int64_t)c.batch * c.kv_heads * (max_len + 2 * moves + 1) * 4;
+  return (int64_t)c.batch * c.kv_heads * list_words(max_len, budget) * 4;
 }
 
 hipError_t launch_cache_evict(const EvictLaunch& a, hipStream_t s) {
   const int64_t moves = most_moves(a.max_len, a.budget);
-  cache_select_kernel<<<dim3(a.c.kv_heads, a.c.batch), kSelectThreads, 0, s>>>(a, moves);
+  const dim3 heads(a.c.kv_heads, a.c.batch);
+  if (a.max_len <= 1024) {
+    cache_select_kernel<256, 4><<<heads, 256, 0, s>>>(a, moves);
+  } else if (a.max_len <= 4096) {
+    cache_select_kernel<256, 16><<<heads, 256, 0, s>>>(a, moves);
+  } else if (a.max_len <= kShortSlots) {
+    cache_select_kernel<1024, 8><<<heads, 1024, 0, s>>>(a, moves);
+  } else {
+    const dim3 grid((unsigned)chunks_of(a.max_len), a.c.kv_heads, a.c.batch);
+    if (moves > 0) {
+      cache_count_kernel<0><<<grid, kChunkThreads, 0, s>>>(a, moves);
+      cache_count_kernel<1><<<grid, kChunkThreads, 0, s>>>(a, moves);
+      cache_count_kernel<2><<<grid, kChunkThreads, 0, s>>>(a, moves);
+    }
+    cache_number_kernel<<<grid, kChunkThreads, 0, s>>>(a, moves);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int32_t per_block = 64;

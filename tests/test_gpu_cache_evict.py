@@ -94,6 +94,41 @@ def test_long(kv, dim, cache):
     check(c, old, 33333, 1111, kept)
 
 
+@pytest.mark.parametrize("slots", (1024, 1040, 4096, 4112, 8192, 8208, 16400))
+@pytest.mark.parametrize("fewer", (1, 4, 5, 600))
+def test_where_the_kernels_change(slots, fewer):
+    """A full table of as many slots as one workgroup takes and one page more,
+    with few and many evictions; other sequences are shorter, one stays whole."""
+    lengths = (slots, slots - fewer, slots - fewer + 1, 700, slots - 1)
+    c = filled(lengths, 2, 8, 16, "bf16", 27, weights="ties")
+    budget = slots - fewer
+    for apart in (False, True):
+        old = clone(c)
+        kept = torch.full((5, 2, budget), -9, dtype=torch.int32, device="cuda")
+        new = dict(new_state=torch.zeros_like(c.state), new_weights=torch.full_like(c.weights, -1.0),
+                   new_order=torch.full_like(c.order, -1)) if apart else {}
+        m.mosaic_cache_evict(c, budget, 3, kept=kept, **new)
+        check(c, old, budget, 3, kept, state=new.get("new_state"), weights=new.get("new_weights"),
+              order=new.get("new_order"))
+        c = old
+
+
+def test_no_pages():
+    """A pool without pages: nothing is there to evict, lengths are cut."""
+    empty = torch.empty((0, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    numbers = torch.empty((0, 2, 16), device="cuda")
+    c = m.KVCache(empty, empty, torch.full((2, 3), -1, dtype=torch.int32, device="cuda"),
+                  torch.tensor([[40, 5], [40, 5]], dtype=torch.int32, device="cuda"), numbers, numbers.int())
+    m.mosaic_cache_evict(c, 20, 3)
+    assert c.state.tolist() == [[20, 5], [40, 5]]
+    q = torch.ones((2, 256), device="cuda")
+    out = torch.ones_like(q)
+    m.mosaic_cache_attend(c, q, 4, out)
+    assert not out.any()
+    m.mosaic_cache_append(c, torch.ones((2, 512), device="cuda"), 4, out)
+    assert c.state.tolist() == [[21, 6], [41, 6]] and torch.equal(out, q)
+
+
 def test_apart():
     """State, weights and order written elsewhere: the same call can be made
     again with the same result."""
