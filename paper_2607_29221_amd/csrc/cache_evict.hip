@@ -164,7 +164,7 @@ __device__ __forceinline__ void load_tokens(const EvictLaunch& a, int b, int h, 
 // Numbers the slots first .. of a workgroup, of which `above` lower ones have
 // a key over `least` and `equal` a key like it (of those `need` stay), and
 // writes the lists. cnt: THREADS / 64 * R words.
-template <int THREADS, int R, bool LOADED>
+template <int THREADS, int R>
 __device__ __forceinline__ void number_slots(const EvictLaunch& a, int b, int h, const Lists& l, int32_t* kept, bool apart,
                                              int32_t first, int32_t n, uint32_t least, uint32_t need, uint32_t above,
                                              uint32_t equal, const Tokens<R>& t, uint32_t* cnt) {
@@ -215,12 +215,8 @@ __device__ __forceinline__ void number_slots(const EvictLaunch& a, int b, int h,
     if (i < budget && in) {
       if (!stays) {
         l.free_slots[i - rank] = i;
-      } else if (LOADED) {
-        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
       } else {
-        const int32_t page = apart ? page_of(a.c, b, i) : -1;
-        const int64_t row = page >= 0 ? row_index(a.c, page, h, i) : -1;
-        stay(a, kept, apart, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
+        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
       }
     } else if (stays) {
       l.movers[budget - 1 - rank] = i;
@@ -336,7 +332,7 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
     need = found[1];
     __syncthreads();
   }
-  number_slots<THREADS, R, true>(a, b, h, l, kept, apart, 0, n, prefix, need, 0u, 0u, t, cnt);
+  number_slots<THREADS, R>(a, b, h, l, kept, apart, 0, n, prefix, need, 0u, 0u, t, cnt);
 }
 
 // Long sequences: the counts of digit D, in chunks of slots.
@@ -368,7 +364,7 @@ __global__ __launch_bounds__(kChunkThreads) void cache_count_kernel(EvictLaunch 
   if (D > 0) {
     const int chunks = (n + kChunk - 1) / kChunk;
     uint32_t own[PER] = {};
-#pragma unroll 8
+#pragma unroll 16
     for (int c = 0; c < chunks; ++c)
 #pragma unroll
       for (int k = 0; k < PER; ++k) own[k] += l.counts[D - 1][(int64_t)c * kBins + kBins - 1 - PER * tid - k];
@@ -428,12 +424,18 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
   }
   if (first >= n) return;
   Tokens<kChunkKeys> t;
+  int32_t page[kChunkKeys];
+  const bool copies = apart && first < a.budget;
 #pragma unroll
-  for (int r = 0; r < kChunkKeys; ++r) t.key[r] = l.keys[min(first + kChunkThreads * r + tid, n - 1)];
+  for (int r = 0; r < kChunkKeys; ++r) {
+    const int32_t i = min(first + kChunkThreads * r + tid, n - 1);
+    t.key[r] = l.keys[i];
+    page[r] = copies ? page_of(a.c, b, i) : -1;
+  }
   // the last digit, and how many of its values lie in the chunks before
   const int chunks = (n + kChunk - 1) / kChunk;
   uint32_t own[PER] = {}, earlier[PER] = {}, above = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int c = 0; c < chunks; ++c)
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -442,6 +444,12 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
       earlier[k] += c < chunk ? v : 0u;
     }
   for (int c = tid; c < chunk; c += kChunkThreads) above += l.above[c];
+#pragma unroll
+  for (int r = 0; r < kChunkKeys; ++r) {          // under way while the digit is found
+    t.row[r] = page[r] >= 0 ? row_index(a.c, page[r], h, min(first + kChunkThreads * r + tid, n - 1)) : -1;
+    t.w[r] = page[r] >= 0 ? a.c.weights[t.row[r]] : 0.0f;
+    t.o[r] = page[r] >= 0 ? a.c.order[t.row[r]] : 0;
+  }
   find_digit<kChunkThreads>(own, l.found[3], part, found);
   const uint32_t digit = found[0], need = found[1], least = l.found[2] << 10 | digit;
 #pragma unroll
@@ -461,7 +469,7 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
     lower[0] = above;
   }
   __syncthreads();
-  number_slots<kChunkThreads, kChunkKeys, false>(a, b, h, l, kept, apart, first, n, least, need, lower[0], lower[1], t, cnt);
+  number_slots<kChunkThreads, kChunkKeys>(a, b, h, l, kept, apart, first, n, least, need, lower[0], lower[1], t, cnt);
 }
 
 // Copies rows along the pairs of slots, 16 bytes per thread.
@@ -509,7 +517,7 @@ hipError_t launch_cache_evict(const EvictLaunch& a, hipStream_t s) {
   if (a.max_len <= 1024) {
     cache_select_kernel<256, 4><<<heads, 256, 0, s>>>(a, moves);
   } else if (a.max_len <= 4096) {
-    cache_select_kernel<256, 16><<<heads, 256, 0, s>>>(a, moves);
+    cache_select_kernel<512, 8><<<heads, 512, 0, s>>>(a, moves);
   } else if (a.max_len <= kShortSlots) {
     cache_select_kernel<1024, 8><<<heads, 1024, 0, s>>>(a, moves);
   } else {
