@@ -47,6 +47,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, in
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, bytes, 0x00020000);
 }
 constexpr int kNowhere = 0x40000000;      // an offset past every page
+constexpr int kStream = 2;                // cache policy: read once, not to be kept
 
 // max or sum over the four lanes of a head (lane mod 16)
 __device__ __forceinline__ float head_max(float v) {
@@ -119,7 +120,7 @@ __device__ __forceinline__ void split(float x, T* part) {
 struct Work {
   float* stat;      // [batch][heads][pieces][2]
   float* part;      // [batch][heads][pieces][head_dim]
-  float* scores;    // [batch][heads][row]
+  float* scores;    // [batch][kv_heads][row / 16][group][16]: what a wave stores at a time lies together
   int64_t row;
   int32_t pieces;
   int32_t piece;    // tokens of a piece
@@ -137,8 +138,9 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len, int32_t accumul
   p.tiles_per_wg = p.head_tiles == 1 ? 1 : p.head_tiles == 2 ? 2 : 4;
   const int64_t groups = (int64_t)c.batch * c.kv_heads * ((p.head_tiles + p.tiles_per_wg - 1) / p.tiles_per_wg);
   const int64_t step = 32 * kWaves / p.tiles_per_wg;
-  // workgroups for every compute unit a few times over, of at least one step
-  const int64_t wanted = (1536 + groups - 1) / groups;
+  // One sequence: as many workgroups as run at once. Several, of lengths that
+  // only the device knows: four times as many, so that short ones even out.
+  const int64_t wanted = ((c.batch == 1 ? 512 : 2048) + groups - 1) / groups;
   int64_t piece = (max_len + wanted - 1) / wanted;
   piece = (piece + step - 1) / step * step;
   if (piece < step) piece = step;
@@ -167,14 +169,23 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   typedef Matrix<CT> M;
   constexpr int E = F::kWide ? 4 : 8;           // elements of a 16-byte key chunk
   constexpr int NV = F::kValueLoads, EV = F::kEach;
-  __shared__ float slab[kWaves][kHeadTile][DP + 4];
+  constexpr int kHold = 8192 / 16;              // of a wave's scores, 16 bytes each
+  union Shared {
+    float slab[kWaves][kHeadTile][DP + 4];      // outputs of the waves, at the end
+    f32x4 held[kWaves][kHold];                  // scores on their way to memory
+  };
+  __shared__ Shared shared;
+  auto& slab = shared.slab;
   __shared__ float stat[kWaves][kHeadTile][2];
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int piece = blockIdx.x, b = blockIdx.z;
-  const int tile_groups = gridDim.y / a.c.kv_heads;
-  const int h = blockIdx.y / tile_groups, tile = (blockIdx.y % tile_groups) * tiles_per_wg + wave % tiles_per_wg;
+  // Workgroups go to the XCDs in turn: pieces come last, so that the early
+  // ones, which every sequence has, start first, and turn the sequences round,
+  // so that no XCD has the long ones to itself.
+  const int piece = blockIdx.z, b = (blockIdx.y + blockIdx.z) % a.c.batch;
+  const int tile_groups = gridDim.x / a.c.kv_heads;
+  const int h = blockIdx.x / tile_groups, tile = (blockIdx.x % tile_groups) * tiles_per_wg + wave % tiles_per_wg;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int n = held_tokens(a.lengths, b, a.max_len);
   const int t0 = piece * wk.piece, t1 = min(n, t0 + wk.piece);
@@ -256,9 +267,23 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
     for (int j = 0; j < EV; ++j) acc[v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float top = -INFINITY, base = 0.0f, sum = 0.0f;
 
-  typename M::Frag key[F::kSub][F::kKeyLoads];
   const int stride = F::kTokens * lanes_of_tokens;
-  const int first = t0 + F::kTokens * (wave / tiles_per_wg);
+  const int first_of_wave = t0 + F::kTokens * (wave / tiles_per_wg);
+
+  // Scores go to memory through LDS, many steps at a time: a load that is
+  // issued behind a store waits for it, and stores take longer than loads.
+  float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 16 * head + 4 * quad;
+  const int tile_heads = min(max(group - tile * kHeadTile, 1), kHeadTile);
+  f32x4* held = &shared.held[wave][quad * tile_heads + min(col, tile_heads - 1)];
+  int holding = 0, held_from = first_of_wave;   // blocks of 16 tokens, and the first one's step
+  auto release = [&]() {
+    if (live)
+      for (int k = 0; k < holding; ++k)
+        *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * stride + k % F::kSub * 16) * group) = held[4 * tile_heads * k];
+    held_from += holding / F::kSub * stride;
+    holding = 0;
+  };
+  typename M::Frag key[F::kSub][F::kKeyLoads];
   Block cur[F::kSub];
   auto load_keys = [&](const Block* k) {
 #pragma unroll
@@ -267,14 +292,14 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
 #pragma unroll
       for (int c = 0; c < F::kKeyLoads; ++c)
         key[s][c] = __builtin_bit_cast(typename M::Frag,
-                                       __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, 0));
+                                       __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, kStream));
     }
   };
 #pragma unroll
-  for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
+  for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first_of_wave + 16 * s);
   load_keys(cur);
 
-  for (int t = first; t < t1; t += stride) {
+  for (int t = first_of_wave; t < t1; t += stride) {
     // values of these tokens, keys of the next ones: in flight during the arithmetic
     u32x4 value[F::kRows][NV];
 #pragma unroll
@@ -286,10 +311,10 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
         for (int v = 0; v < NV; ++v) {
           if (EV * sizeof(C) == 16) {
             value[4 * s + i][v] =
-                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, 0));
+                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kStream));
           } else {
             const u32x2 w =
-                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, 0));
+                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kStream));
             value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
           }
         }
@@ -312,11 +337,15 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
         p[4 * s + i] = 4 * quad + i < cur[s].valid ? dot[i] * scale : -INFINITY;
         tile_top = fmaxf(tile_top, p[4 * s + i]);
       }
-      if (a.accumulate && live)
-        *(f32x4*)(wk.scores + ((int64_t)b * a.heads + h * group + head) * wk.row + t + 16 * s + 4 * quad) =
-            f32x4{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
     }
     load_keys(next);
+    if (a.accumulate) {
+      if (4 * tile_heads * (holding + F::kSub) > kHold) release();
+#pragma unroll
+      for (int s = 0; s < F::kSub; ++s)
+        if (live) held[4 * tile_heads * (holding + s)] = f32x4{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
+      holding += F::kSub;
+    }
 
     if (__any(tile_top > top + F::kSlack)) {
       const float now = fmaxf(top, head_max(tile_top));
@@ -363,6 +392,8 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
     for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
   }
 
+  if (a.accumulate) release();
+
   // join the waves that share heads
   sum = head_sum(sum);
   if (quad == 0) {
@@ -387,7 +418,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   const int chunks = D / 4;
   for (int u = tid; u < tiles_per_wg * kHeadTile * chunks; u += 64 * kWaves) {
     const int hd = u / chunks, c = u - hd * chunks, w0 = hd / kHeadTile, hc = hd % kHeadTile;
-    const int g = ((blockIdx.y % tile_groups) * tiles_per_wg + w0) * kHeadTile + hc;
+    const int g = ((blockIdx.x % tile_groups) * tiles_per_wg + w0) * kHeadTile + hc;
     if (g >= group) continue;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     float common = -INFINITY, total = 0.0f;
@@ -430,18 +461,18 @@ __device__ __forceinline__ void head_norm(const float* st, int pieces, int lane,
 // query head's output each: rows of 16-byte columns, the pieces dealt out to
 // the rows of threads. The others add the weights of kJoinTokens tokens up,
 // over the heads of the group.
-constexpr int kJoinHeads = 16, kJoinTokens = 1024;
+constexpr int kJoinHeads = 16, kJoinTokens = 4 * 256;
 template <int XT>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk) {
   typedef typename FloatType<XT>::type X;
   __shared__ f32x4 rows[256];
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.y, b = blockIdx.z, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
+  const int h = blockIdx.x, b = blockIdx.y, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int n = held_tokens(a.lengths, b, a.max_len);
   const int pieces = n == 0 ? 1 : (n + wk.piece - 1) / wk.piece;
-  if ((int)blockIdx.x < group) {
-    const int64_t row = (int64_t)b * a.heads + h * group + blockIdx.x;
+  if ((int)blockIdx.z < group) {
+    const int64_t row = (int64_t)b * a.heads + h * group + blockIdx.z;
     const float* st = wk.stat + 2 * row * wk.pieces;
     float common, sum;
     head_norm(st, pieces, lane, &common, &sum);   // every wave for itself
@@ -458,14 +489,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
     if (tid >= cols) return;
     for (int s = 1; s < at_once; ++s) o += rows[s * cols + tid];
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + blockIdx.x) * D + 4 * tid;
+    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + blockIdx.z) * D + 4 * tid;
 #pragma unroll
     for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
     return;
   }
-  const int t0 = ((int)blockIdx.x - group) * kJoinTokens;
+  const int t0 = ((int)blockIdx.z - group) * kJoinTokens;
   if (t0 >= n) return;
-  float w[kJoinTokens / 256] = {};
+  const int t = t0 + 4 * tid;                     // four tokens of one page
+  const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
+  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
     const int count = min(group - g0, kJoinHeads);
     const int64_t row0 = (int64_t)b * a.heads + h * group + g0;
@@ -479,18 +512,24 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
       }
     }
     __syncthreads();
+    if (t < n) {
+#pragma unroll 8
+      for (int g = 0; g < count; ++g) {
+        const f32x4 score = *(const f32x4*)(scores + 16 * (g0 + g));
 #pragma unroll
-    for (int k = 0; k < kJoinTokens / 256; ++k) {
-      const int t = t0 + 256 * k + tid;
-      if (t < n)
-        for (int g = 0; g < count; ++g) w[k] += exp2_fast(wk.scores[(row0 + g) * wk.row + t] - norm[g][0]) * norm[g][1];
+        for (int i = 0; i < 4; ++i) w[i] += exp2_fast(score[i] - norm[g][0]) * norm[g][1];
+      }
     }
   }
+  const int page = t < n ? page_of(a.c, b, t) : -1;
+  if (page < 0) return;
+  float* dst = a.c.weights + row_index(a.c, page, h, t);
+  if (t + 4 <= n) {
+    *(f32x4_any*)dst += w;
+  } else {
 #pragma unroll
-  for (int k = 0; k < kJoinTokens / 256; ++k) {
-    const int t = t0 + 256 * k + tid;
-    const int page = t < n ? page_of(a.c, b, t) : -1;
-    if (page >= 0) a.c.weights[row_index(a.c, page, h, t)] += w[k];
+    for (int i = 0; i < 3; ++i)
+      if (t + i < n) dst[i] += w[i];
   }
 }
 
@@ -503,13 +542,13 @@ hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
     w.part = w.stat + stat_floats(a.c, a.heads, p);
     w.scores = w.part + part_floats(a.c, a.heads, p);
   }
-  const dim3 grid(p.pieces, a.c.kv_heads * ((p.head_tiles + p.tiles_per_wg - 1) / p.tiles_per_wg), a.c.batch);
+  const dim3 grid(a.c.kv_heads * ((p.head_tiles + p.tiles_per_wg - 1) / p.tiles_per_wg), a.c.batch, p.pieces);
   if (a.c.head_dim <= 64) cache_attend_kernel<CT, XT, 64><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
   else if (a.c.head_dim <= 128) cache_attend_kernel<CT, XT, 128><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
   else cache_attend_kernel<CT, XT, 256><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
   if (p.join) {
     const int64_t ranges = a.accumulate ? (a.max_len + kJoinTokens - 1) / kJoinTokens : 0;
-    cache_join_kernel<XT><<<dim3((unsigned)(a.heads / a.c.kv_heads + ranges), a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, w);
+    cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, (unsigned)(a.heads / a.c.kv_heads + ranges)), 256, 0, s>>>(a, w);
   }
   return hipGetLastError();
 }
