@@ -63,6 +63,14 @@ __device__ __forceinline__ float head_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Every wave's writes to LDS before every wave's reads after; memory accesses
+// go on (a __syncthreads waits for those too).
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // What the types of cache and activations make of a wave's step. DP: head_dim
@@ -128,16 +136,18 @@ struct Work {
 
 struct Plan {
   int32_t pieces, piece;
-  int32_t head_tiles, tiles_per_wg;       // blocks of 16 query heads of a group
+  int32_t wave_tiles, tile_groups;        // blocks of 16 query heads of a group: per wave, and so many times
   bool join;
 };
 
 Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len, int32_t accumulate) {
   Plan p;
-  p.head_tiles = (heads / c.kv_heads + kHeadTile - 1) / kHeadTile;
-  p.tiles_per_wg = p.head_tiles == 1 ? 1 : p.head_tiles == 2 ? 2 : 4;
-  const int64_t groups = (int64_t)c.batch * c.kv_heads * ((p.head_tiles + p.tiles_per_wg - 1) / p.tiles_per_wg);
-  const int64_t step = 32 * kWaves / p.tiles_per_wg;
+  const int32_t tiles = (heads / c.kv_heads + kHeadTile - 1) / kHeadTile;
+  // two blocks share a wave's keys and values where the registers hold both outputs
+  p.wave_tiles = tiles > 1 && c.head_dim <= 128 ? 2 : 1;
+  p.tile_groups = (tiles + p.wave_tiles - 1) / p.wave_tiles;
+  const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tile_groups;
+  const int64_t step = 32 * kWaves;
   // One sequence: as many workgroups as run at once. Several, of lengths that
   // only the device knows: four times as many, so that short ones even out.
   const int64_t wanted = ((c.batch == 1 ? 512 : 2048) + groups - 1) / groups;
@@ -160,23 +170,28 @@ int64_t part_floats(const CacheView& c, int32_t heads, const Plan& p) {
   return (int64_t)c.batch * heads * p.pieces * c.head_dim;
 }
 
-template <int CT, int XT, int DP>
-__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_kernel(AttendLaunch a, Work wk,
-                                                                                      int32_t tiles_per_wg, bool join) {
+// NT: blocks of 16 query heads per wave. STREAM: no other workgroup reads the
+// same keys and values.
+template <int CT, int XT, int DP, int NT, bool STREAM>
+__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_kernel(AttendLaunch a, Work wk, bool join) {
   typedef Form<CT, XT, DP> F;
   typedef typename F::C C;
   typedef typename F::X X;
   typedef Matrix<CT> M;
+  typedef typename M::Frag Frag;
   constexpr int E = F::kWide ? 4 : 8;           // elements of a 16-byte key chunk
-  constexpr int NV = F::kValueLoads, EV = F::kEach;
+  constexpr int KL = F::kKeyLoads, NV = F::kValueLoads, EV = F::kEach, PARTS = F::kParts;
+  constexpr int kPolicy = STREAM ? kStream : 0;
   constexpr int kHold = 8192 / 16;              // of a wave's scores, 16 bytes each
   union Shared {
+    struct {
+      Frag query[NT][PARTS][KL][64];            // operands of the first product, by lane
+      f32x4 held[kWaves][kHold];                // scores on their way to memory
+    } in;
     float slab[kWaves][kHeadTile][DP + 4];      // outputs of the waves, at the end
-    f32x4 held[kWaves][kHold];                  // scores on their way to memory
   };
   __shared__ Shared shared;
-  auto& slab = shared.slab;
-  __shared__ float stat[kWaves][kHeadTile][2];
+  __shared__ float stat[NT][kWaves][kHeadTile][2];
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -185,57 +200,17 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   // so that no XCD has the long ones to itself.
   const int piece = blockIdx.z, b = (blockIdx.y + blockIdx.z) % a.c.batch;
   const int tile_groups = gridDim.x / a.c.kv_heads;
-  const int h = blockIdx.x / tile_groups, tile = (blockIdx.x % tile_groups) * tiles_per_wg + wave % tiles_per_wg;
+  const int h = blockIdx.x / tile_groups, tile0 = blockIdx.x % tile_groups * NT;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int n = held_tokens(a.lengths, b, a.max_len);
   const int t0 = piece * wk.piece, t1 = min(n, t0 + wk.piece);
-  const int lanes_of_tokens = kWaves / tiles_per_wg;
   if (t0 > 0 && t0 >= n) return;                // pieces past the end are not read back
-
-  // queries of head `head` of the group: operand of the first product, in parts
-  const int head = tile * kHeadTile + col;
-  const bool live = head < group;
-  typename M::Frag q[F::kParts][F::kKeyLoads];
-  float scale = a.scale_log2;
-  {
-    const X* row = (const X*)((const char*)a.q + (int64_t)b * a.ldq) + ((int64_t)h * group + head) * D;
-    float x[F::kKeyLoads][E];
-    float top = 0.0f;
-#pragma unroll
-    for (int c = 0; c < F::kKeyLoads; ++c) {
-      const int d = (4 * c + quad) * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        x[c][e] = live && d < D ? (float)row[d + e] : 0.0f;
-        top = fmaxf(top, fabsf(x[c][e]));
-      }
-    }
-    if (CT == MOSAIC_F16 && XT == MOSAIC_F32) {
-      // by a power of two into the upper part of the range of f16
-      top = head_max(top);
-      const int up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
-      scale = ldexpf(scale, -up);
-#pragma unroll
-      for (int c = 0; c < F::kKeyLoads; ++c)
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[c][e] = ldexpf(x[c][e], up);
-    }
-#pragma unroll
-    for (int c = 0; c < F::kKeyLoads; ++c)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        C part[F::kParts];
-        split<C, F::kParts>(x[c][e], part);
-#pragma unroll
-        for (int s = 0; s < F::kParts; ++s) q[s][c][e] = part[s];
-      }
-  }
 
   // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
   const int ts = (int)a.c.token_stride;
-  int key_off[F::kKeyLoads], value_off[NV];
+  int key_off[KL], value_off[NV];
 #pragma unroll
-  for (int c = 0; c < F::kKeyLoads; ++c) key_off[c] = (4 * c + quad) * E < D ? col * ts + (4 * c + quad) * 16 : kNowhere;
+  for (int c = 0; c < KL; ++c) key_off[c] = (4 * c + quad) * E < D ? col * ts + (4 * c + quad) * 16 : kNowhere;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int d = (16 * v + col) * EV;
@@ -259,47 +234,97 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
     }
     return k;
   };
-
-  f32x4 acc[NV][EV];
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int j = 0; j < EV; ++j) acc[v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float top = -INFINITY, base = 0.0f, sum = 0.0f;
-
-  const int stride = F::kTokens * lanes_of_tokens;
-  const int first_of_wave = t0 + F::kTokens * (wave / tiles_per_wg);
-
-  // Scores go to memory through LDS, many steps at a time: a load that is
-  // issued behind a store waits for it, and stores take longer than loads.
-  float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 16 * head + 4 * quad;
-  const int tile_heads = min(max(group - tile * kHeadTile, 1), kHeadTile);
-  f32x4* held = &shared.held[wave][quad * tile_heads + min(col, tile_heads - 1)];
-  int holding = 0, held_from = first_of_wave;   // blocks of 16 tokens, and the first one's step
-  auto release = [&]() {
-    if (live)
-      for (int k = 0; k < holding; ++k)
-        *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * stride + k % F::kSub * 16) * group) = held[4 * tile_heads * k];
-    held_from += holding / F::kSub * stride;
-    holding = 0;
-  };
-  typename M::Frag key[F::kSub][F::kKeyLoads];
-  Block cur[F::kSub];
+  Frag key[F::kSub][KL];
   auto load_keys = [&](const Block* k) {
 #pragma unroll
     for (int s = 0; s < F::kSub; ++s) {
       const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.k + k[s].base, k[s].valid * ts);
 #pragma unroll
-      for (int c = 0; c < F::kKeyLoads; ++c)
-        key[s][c] = __builtin_bit_cast(typename M::Frag,
-                                       __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, kStream));
+      for (int c = 0; c < KL; ++c)
+        key[s][c] = __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, kPolicy));
     }
   };
+  constexpr int kStep = F::kTokens * kWaves;
+  const int first = t0 + F::kTokens * wave;
+  Block cur[F::kSub];
 #pragma unroll
-  for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first_of_wave + 16 * s);
+  for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
   load_keys(cur);
 
-  for (int t = first_of_wave; t < t1; t += stride) {
+  // Queries, in parts: every wave reads them (the scale is a lane's own) and
+  // writes a share.
+  float scale[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int head = (tile0 + nt) * kHeadTile + col;
+    const X* row = (const X*)((const char*)a.q + (int64_t)b * a.ldq) + ((int64_t)h * group + head) * D;
+    float x[KL][E];
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < KL; ++c) {
+      const int d = (4 * c + quad) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[c][e] = head < group && d < D ? (float)row[d + e] : 0.0f;
+        top = fmaxf(top, fabsf(x[c][e]));
+      }
+    }
+    int up = 0;
+    if (CT == MOSAIC_F16 && XT == MOSAIC_F32) {
+      // by a power of two into the upper part of the range of f16
+      top = head_max(top);
+      up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+    }
+    scale[nt] = ldexpf(a.scale_log2, -up);
+#pragma unroll
+    for (int c = 0; c < KL; ++c) {
+      if (c % kWaves != wave) continue;
+      Frag f[PARTS];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        C part[PARTS];
+        split<C, PARTS>(CT == MOSAIC_F16 && XT == MOSAIC_F32 ? ldexpf(x[c][e], up) : x[c][e], part);
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
+      }
+#pragma unroll
+      for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][lane] = f[s];
+    }
+  }
+  lds_barrier();                                // leaves the keys under way
+
+  f32x4 acc[NT][NV][EV];
+  float top[NT], base[NT], sum[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    top[nt] = -INFINITY;
+    base[nt] = sum[nt] = 0.0f;
+  }
+
+  // Scores go to memory through LDS, many steps at a time: a load that is
+  // issued behind a store waits for it, and stores take longer than loads.
+  float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 4 * quad;
+  const int held_heads = min(group - tile0 * kHeadTile, NT * kHeadTile);
+  int holding = 0, held_from = first;           // blocks of 16 tokens, and the first one's step
+  auto release = [&]() {
+    for (int k = 0; k < holding; ++k)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int hd = nt * kHeadTile + col;
+        if (hd < held_heads)
+          *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group + 16 * (tile0 * kHeadTile + hd)) =
+              shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
+      }
+    held_from += holding / F::kSub * kStep;
+    holding = 0;
+  };
+
+  for (int t = first; t < t1; t += kStep) {
+    asm volatile("" ::: "memory");              // the queries stay in LDS
     // values of these tokens, keys of the next ones: in flight during the arithmetic
     u32x4 value[F::kRows][NV];
 #pragma unroll
@@ -311,70 +336,87 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
         for (int v = 0; v < NV; ++v) {
           if (EV * sizeof(C) == 16) {
             value[4 * s + i][v] =
-                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kStream));
+                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kPolicy));
           } else {
             const u32x2 w =
-                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kStream));
+                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kPolicy));
             value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
           }
         }
     }
     Block next[F::kSub];
 #pragma unroll
-    for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + stride + 16 * s);
+    for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
 
-    float p[F::kRows];
-    float tile_top = -INFINITY;
+    float p[NT][F::kRows], tile_top[NT];
 #pragma unroll
-    for (int s = 0; s < F::kSub; ++s) {
-      f32x4 dot = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int nt = 0; nt < NT; ++nt) {
+      f32x4 dot[F::kSub];
 #pragma unroll
-      for (int part = F::kParts - 1; part >= 0; --part)       // small terms first
+      for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int c = 0; c < F::kKeyLoads; ++c) dot = M::mul(key[s][c], q[part][c], dot);
+      for (int part = PARTS - 1; part >= 0; --part)           // small terms first
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[4 * s + i] = 4 * quad + i < cur[s].valid ? dot[i] * scale : -INFINITY;
-        tile_top = fmaxf(tile_top, p[4 * s + i]);
-      }
+        for (int c = 0; c < KL; ++c) {
+          const Frag q = shared.in.query[nt][part][c][lane];
+#pragma unroll
+          for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
+        }
+      tile_top[nt] = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < F::kSub; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * scale[nt] : -INFINITY;
+          tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
+        }
     }
     load_keys(next);
     if (a.accumulate) {
-      if (4 * tile_heads * (holding + F::kSub) > kHold) release();
+      if (4 * held_heads * (holding + F::kSub) > kHold) release();
 #pragma unroll
-      for (int s = 0; s < F::kSub; ++s)
-        if (live) held[4 * tile_heads * (holding + s)] = f32x4{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s) {
+          const int hd = nt * kHeadTile + col;
+          if (hd < held_heads)
+            shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
+                f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
+        }
       holding += F::kSub;
     }
 
-    if (__any(tile_top > top + F::kSlack)) {
-      const float now = fmaxf(top, head_max(tile_top));
-      const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
-      const float f = top == -INFINITY ? 0.0f : exp2_fast(base - rescaled);
-      sum *= f;
+    Frag pf[NT][PARTS];
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+    for (int nt = 0; nt < NT; ++nt) {
+      if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
+        const float now = fmaxf(top[nt], head_max(tile_top[nt]));
+        const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
+        const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - rescaled);
+        sum[nt] *= f;
 #pragma unroll
-        for (int j = 0; j < EV; ++j) acc[v][j] *= f;
-      top = now;
-      base = rescaled;
-    }
-    typename M::Frag pf[F::kParts];
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int i = 0; i < F::kRows; ++i) {
-      const float w = exp2_fast(p[i] - base);
-      sum += w;
-      C part[F::kParts];
-      split<C, F::kParts>(w, part);
+          for (int j = 0; j < EV; ++j) acc[nt][v][j] *= f;
+        top[nt] = now;
+        base[nt] = rescaled;
+      }
 #pragma unroll
-      for (int s = 0; s < F::kParts; ++s) pf[s][i] = part[s];
+      for (int i = 0; i < F::kRows; ++i) {
+        const float w = exp2_fast(p[nt][i] - base[nt]);
+        sum[nt] += w;
+        C part[PARTS];
+        split<C, PARTS>(w, part);
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) pf[nt][s][i] = part[s];
+      }
     }
 
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int j = 0; j < EV; ++j) {
-        typename M::Frag vf;
+        Frag vf;
         if constexpr (F::kWide) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
@@ -383,63 +425,72 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-          vf = __builtin_bit_cast(typename M::Frag, w);
+          vf = __builtin_bit_cast(Frag, w);
         }
 #pragma unroll
-        for (int part = F::kParts - 1; part >= 0; --part) acc[v][j] = M::mul(vf, pf[part], acc[v][j]);
+        for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
       }
 #pragma unroll
     for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
   }
-
   if (a.accumulate) release();
 
-  // join the waves that share heads
-  sum = head_sum(sum);
-  if (quad == 0) {
-    stat[wave][col][0] = top == -INFINITY ? -INFINITY : base;
-    stat[wave][col][1] = sum;
-  }
-  __syncthreads();
-  {
-    float common = -INFINITY;
-    for (int w = wave % tiles_per_wg; w < kWaves; w += tiles_per_wg) common = fmaxf(common, stat[w][col][0]);
-    const float f = stat[wave][col][0] == -INFINITY ? 0.0f : exp2_fast(base - common);
+  // join the waves
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < EV; j += 4)
-          *(f32x4*)&slab[wave][col][(16 * v + 4 * quad + i) * EV + j] =
-              f32x4{acc[v][j][i] * f, acc[v][j + 1][i] * f, acc[v][j + 2][i] * f, acc[v][j + 3][i] * f};
-  }
-  __syncthreads();
-  const int chunks = D / 4;
-  for (int u = tid; u < tiles_per_wg * kHeadTile * chunks; u += 64 * kWaves) {
-    const int hd = u / chunks, c = u - hd * chunks, w0 = hd / kHeadTile, hc = hd % kHeadTile;
-    const int g = ((blockIdx.x % tile_groups) * tiles_per_wg + w0) * kHeadTile + hc;
-    if (g >= group) continue;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    float common = -INFINITY, total = 0.0f;
-    for (int w = w0; w < kWaves; w += tiles_per_wg) {
-      o += *(const f32x4*)&slab[w][hc][4 * c];
-      common = fmaxf(common, stat[w][hc][0]);
+  for (int nt = 0; nt < NT; ++nt) {
+    const float all = head_sum(sum[nt]);
+    if (quad == 0) {
+      stat[nt][wave][col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
+      stat[nt][wave][col][1] = all;
     }
-    for (int w = w0; w < kWaves; w += tiles_per_wg)
-      total += stat[w][hc][1] * (stat[w][hc][0] == -INFINITY ? 0.0f : exp2_fast(stat[w][hc][0] - common));
-    const int64_t row = (int64_t)b * a.heads + h * group + g;
-    if (join) {
-      *(f32x4*)(wk.part + (row * wk.pieces + piece) * D + 4 * c) = o;
-      if (c == 0) {
-        wk.stat[2 * (row * wk.pieces + piece)] = common;
-        wk.stat[2 * (row * wk.pieces + piece) + 1] = total;
-      }
-    } else {
-      X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g) * D + 4 * c;
-      const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  }
+  const int chunks = D / 4;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
+  for (int nt = 0; nt < NT; ++nt) {
+    __syncthreads();
+    {
+      float common = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stat[nt][w][col][0]);
+      const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - common);
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < EV; j += 4)
+            *(f32x4*)&shared.slab[wave][col][(16 * v + 4 * quad + i) * EV + j] =
+                f32x4{acc[nt][v][j][i] * f, acc[nt][v][j + 1][i] * f, acc[nt][v][j + 2][i] * f, acc[nt][v][j + 3][i] * f};
+    }
+    __syncthreads();
+    const int g0 = (tile0 + nt) * kHeadTile, live = min(group - g0, kHeadTile);
+    for (int u = tid; u < live * chunks; u += 64 * kWaves) {
+      const int hd = u / chunks, c = u - hd * chunks;
+      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+      float common = -INFINITY, total = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        o += *(const f32x4*)&shared.slab[w][hd][4 * c];
+        common = fmaxf(common, stat[nt][w][hd][0]);
+      }
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        total += stat[nt][w][hd][1] * (stat[nt][w][hd][0] == -INFINITY ? 0.0f : exp2_fast(stat[nt][w][hd][0] - common));
+      const int64_t row = (int64_t)b * a.heads + h * group + g0 + hd;
+      if (join) {
+        *(f32x4*)(wk.part + (row * wk.pieces + piece) * D + 4 * c) = o;
+        if (c == 0) {
+          wk.stat[2 * (row * wk.pieces + piece)] = common;
+          wk.stat[2 * (row * wk.pieces + piece) + 1] = total;
+        }
+      } else {
+        X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g0 + hd) * D + 4 * c;
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
+      }
     }
   }
 }
@@ -533,6 +584,22 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
   }
 }
 
+template <int CT, int XT, int DP>
+void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
+  const dim3 grid(a.c.kv_heads * p.tile_groups, a.c.batch, p.pieces), block(64 * kWaves);
+  if constexpr (DP < 256) {
+    if (p.wave_tiles == 2) {
+      if (p.tile_groups == 1) cache_attend_kernel<CT, XT, DP, 2, true><<<grid, block, 0, s>>>(a, w, p.join);
+      else cache_attend_kernel<CT, XT, DP, 2, false><<<grid, block, 0, s>>>(a, w, p.join);
+      return;
+    }
+  } else if (p.tile_groups > 1) {
+    cache_attend_kernel<CT, XT, DP, 1, false><<<grid, block, 0, s>>>(a, w, p.join);
+    return;
+  }
+  cache_attend_kernel<CT, XT, DP, 1, true><<<grid, block, 0, s>>>(a, w, p.join);
+}
+
 template <int CT, int XT>
 hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
   const Plan p = plan_of(a.c, a.heads, a.max_len, a.accumulate);
@@ -542,10 +609,9 @@ hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
     w.part = w.stat + stat_floats(a.c, a.heads, p);
     w.scores = w.part + part_floats(a.c, a.heads, p);
   }
-  const dim3 grid(a.c.kv_heads * ((p.head_tiles + p.tiles_per_wg - 1) / p.tiles_per_wg), a.c.batch, p.pieces);
-  if (a.c.head_dim <= 64) cache_attend_kernel<CT, XT, 64><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
-  else if (a.c.head_dim <= 128) cache_attend_kernel<CT, XT, 128><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
-  else cache_attend_kernel<CT, XT, 256><<<grid, 64 * kWaves, 0, s>>>(a, w, p.tiles_per_wg, p.join);
+  if (a.c.head_dim <= 64) launch_tiles<CT, XT, 64>(a, w, p, s);
+  else if (a.c.head_dim <= 128) launch_tiles<CT, XT, 128>(a, w, p, s);
+  else launch_tiles<CT, XT, 256>(a, w, p, s);
   if (p.join) {
     const int64_t ranges = a.accumulate ? (a.max_len + kJoinTokens - 1) / kJoinTokens : 0;
     cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, (unsigned)(a.heads / a.c.kv_heads + ranges)), 256, 0, s>>>(a, w);
