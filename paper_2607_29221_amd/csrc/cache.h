@@ -88,10 +88,18 @@ template <> struct FloatType<MOSAIC_F32> { typedef float type; };
 template <> struct FloatType<MOSAIC_BF16> { typedef __bf16 type; };
 template <> struct FloatType<MOSAIC_F16> { typedef _Float16 type; };
 
+// Memory that no kernel on the stream writes while this one reads it, at
+// addresses that a wave has in common: through the scalar cache, so the answer
+// does not wait for the vector loads that are under way.
+typedef const __attribute__((address_space(4))) int32_t* uniform_i32;
+
 // Tokens that sequence b holds, as far as slots reach.
+__device__ __forceinline__ int32_t held_of(int32_t n, int64_t most) { return n < 0 ? 0 : n > most ? (int32_t)most : n; }
 __device__ __forceinline__ int32_t held_tokens(const int32_t* lengths, int b, int64_t most) {
-  const int32_t n = lengths[b];
-  return n < 0 ? 0 : n > most ? (int32_t)most : n;
+  return held_of(lengths[b], most);
+}
+__device__ __forceinline__ int32_t held_tokens_uniform(const int32_t* lengths, int b, int64_t most) {
+  return held_of(((uniform_i32)(uintptr_t)lengths)[b], most);
 }
 
 // The page of a slot of sequence b, -1 if it is not there.
@@ -100,10 +108,7 @@ __device__ __forceinline__ int32_t page_of(const CacheView& c, int64_t b, int64_
   return p >= 0 && p < c.pages ? p : -1;
 }
 
-// The same for a slot that the whole wave asks for: through the scalar cache
-// (the table is not written while a kernel reads it), so the answer does not
-// wait for the vector loads that are under way.
-typedef const __attribute__((address_space(4))) int32_t* uniform_i32;
+// The same for a slot that the whole wave asks for.
 __device__ __forceinline__ int32_t page_of_uniform(const CacheView& c, int64_t b, int32_t slot) {
   const int32_t p = ((uniform_i32)(uintptr_t)c.table)[b * c.ldt + (slot >> c.log2_page)];
   return p >= 0 && p < c.pages ? p : -1;

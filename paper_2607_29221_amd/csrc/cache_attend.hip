@@ -63,6 +63,8 @@ __device__ __forceinline__ float head_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+template <class T> struct Chunk { T e[16 / sizeof(T)]; };
+
 // Every wave's writes to LDS before every wave's reads after; memory accesses
 // go on (a __syncthreads waits for those too).
 __device__ __forceinline__ void lds_barrier() {
@@ -202,9 +204,24 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   const int tile_groups = gridDim.x / a.c.kv_heads;
   const int h = blockIdx.x / tile_groups, tile0 = blockIdx.x % tile_groups * NT;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
-  const int n = held_tokens(a.lengths, b, a.max_len);
+  const int n = held_tokens_uniform(a.lengths, b, a.max_len);
   const int t0 = piece * wk.piece, t1 = min(n, t0 + wk.piece);
   if (t0 > 0 && t0 >= n) return;                // pieces past the end are not read back
+
+  // the queries, asked for first (loads come back in order); lanes without a
+  // head or column read another's
+  constexpr int QL = E * (int)sizeof(X) / 16;   // loads per chunk
+  u32x4 raw[NT][KL][QL];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int head = min((tile0 + nt) * kHeadTile + col, group - 1);
+    const char* row = (const char*)a.q + (int64_t)b * a.ldq + ((int64_t)h * group + head) * D * (int)sizeof(X);
+#pragma unroll
+    for (int c = 0; c < KL; ++c)
+#pragma unroll
+      for (int l = 0; l < QL; ++l)
+        raw[nt][c][l] = *(const u32x4*)(row + min((4 * c + quad) * E, D - E) * (int)sizeof(X) + 16 * l);
+  }
 
   // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
   const int ts = (int)a.c.token_stride;
@@ -249,7 +266,29 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   Block cur[F::kSub];
 #pragma unroll
   for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
+  // values of these tokens
+  u32x4 value[F::kRows][NV];
+  auto load_values = [&](const Block* k) {
+#pragma unroll
+    for (int s = 0; s < F::kSub; ++s) {
+      const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.v + k[s].base, k[s].valid * ts);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          if (EV * sizeof(C) == 16) {
+            value[4 * s + i][v] =
+                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kPolicy));
+          } else {
+            const u32x2 w =
+                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kPolicy));
+            value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
+          }
+        }
+    }
+  };
   load_keys(cur);
+  load_values(cur);
 
   // Queries, in parts: every wave reads them (the scale is a lane's own) and
   // writes a share.
@@ -257,15 +296,16 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int head = (tile0 + nt) * kHeadTile + col;
-    const X* row = (const X*)((const char*)a.q + (int64_t)b * a.ldq) + ((int64_t)h * group + head) * D;
     float x[KL][E];
     float top = 0.0f;
 #pragma unroll
     for (int c = 0; c < KL; ++c) {
-      const int d = (4 * c + quad) * E;
+      const bool there = head < group && (4 * c + quad) * E < D;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        x[c][e] = head < group && d < D ? (float)row[d + e] : 0.0f;
+        constexpr int PER = 16 / (int)sizeof(X);
+        const Chunk<X> v = __builtin_bit_cast(Chunk<X>, raw[nt][c][e / PER]);
+        x[c][e] = there ? (float)v.e[e % PER] : 0.0f;
         top = fmaxf(top, fabsf(x[c][e]));
       }
     }
@@ -291,7 +331,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
       for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][lane] = f[s];
     }
   }
-  lds_barrier();                                // leaves the keys under way
+  lds_barrier();                                // leaves keys and values under way
 
   f32x4 acc[NT][NV][EV];
   float top[NT], base[NT], sum[NT];
@@ -325,25 +365,6 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
 
   for (int t = first; t < t1; t += kStep) {
     asm volatile("" ::: "memory");              // the queries stay in LDS
-    // values of these tokens, keys of the next ones: in flight during the arithmetic
-    u32x4 value[F::kRows][NV];
-#pragma unroll
-    for (int s = 0; s < F::kSub; ++s) {
-      const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.v + cur[s].base, cur[s].valid * ts);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          if (EV * sizeof(C) == 16) {
-            value[4 * s + i][v] =
-                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kPolicy));
-          } else {
-            const u32x2 w =
-                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kPolicy));
-            value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
-          }
-        }
-    }
     Block next[F::kSub];
 #pragma unroll
     for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
@@ -434,6 +455,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
       }
 #pragma unroll
     for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
+    load_values(cur);
   }
   if (a.accumulate) release();
 
@@ -520,7 +542,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.x, b = blockIdx.y, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
-  const int n = held_tokens(a.lengths, b, a.max_len);
+  const int n = held_tokens_uniform(a.lengths, b, a.max_len);
   const int pieces = n == 0 ? 1 : (n + wk.piece - 1) / wk.piece;
   if ((int)blockIdx.z < group) {
     const int64_t row = (int64_t)b * a.heads + h * group + blockIdx.z;
