@@ -117,6 +117,8 @@ mosaic_status check_attend(const mosaic_kv_cache* cache, int32_t heads, int64_t 
   a->heads = heads;
   a->max_len = max_len < slots_of(a->c) ? max_len : slots_of(a->c);
   a->accumulate = accumulate != 0;
+  if (a->c.batch > 0 && a->max_len > ((int64_t)1 << 36) / a->c.batch)     // steps of all sequences are counted in 32 bits
+    return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^36 slots");
   return MOSAIC_OK;
 }
 

@@ -24,9 +24,11 @@
 //   matrix cores have room for it (a sixth of their rate at full bandwidth).
 // * M is raised, and O rescaled, only when a score passes it by more than
 //   kSlack: sums of up to 2^kSlack are as exact as sums of up to 1.
-// * Sequences are cut into pieces so that there are workgroups for all
-//   compute units; a second kernel joins the pieces, and adds up attention
-//   weights from the scores that the first one left in the workspace.
+// * All tokens of a key/value head, one sequence after the other, are cut into
+//   equal shares, one per workgroup, from the lengths that the device holds: a
+//   workgroup takes part of one sequence or several. A second kernel joins the
+//   parts, and adds up attention weights from the scores that the first one
+//   left in the workspace.
 #include "cache.h"
 #include "device_common.h"
 #include "dispatch.h"
@@ -125,40 +127,39 @@ __device__ __forceinline__ void split(float x, T* part) {
   }
 }
 
-// The pieces of the workspace: per (sequence, query head, piece) the base and
-// the sum of its weights and its unnormalised output; then scores.
+// Tokens are dealt out in steps of kStepTokens (a sequence's last one may be
+// short). With `total` steps of all sequences, workgroup u of a key/value head
+// takes the steps u * share .. of the sequences laid end to end, share =
+// ceil(total / workgroups). Its part of sequence b has slot u + b: going on, a
+// workgroup or a sequence ends, so no two parts have the same.
+constexpr int kStepTokens = 128;
+
+// The workspace: per slot and query head the base and the sum of the weights
+// and the unnormalised output; then scores.
 struct Work {
-  float* stat;      // [batch][heads][pieces][2]
-  float* part;      // [batch][heads][pieces][head_dim]
+  float* stat;      // [slots][heads][2]
+  float* part;      // [slots][heads][head_dim]
   float* scores;    // [batch][kv_heads][row / 16][group][16]: what a wave stores at a time lies together
   int64_t row;
-  int32_t pieces;
-  int32_t piece;    // tokens of a piece
 };
 
 struct Plan {
-  int32_t pieces, piece;
+  int32_t workgroups;                     // per key/value head and tile group
   int32_t wave_tiles, tile_groups;        // blocks of 16 query heads of a group: per wave, and so many times
-  bool join;
 };
 
-Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len, int32_t accumulate) {
+Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   Plan p;
   const int32_t tiles = (heads / c.kv_heads + kHeadTile - 1) / kHeadTile;
   // two blocks share a wave's keys and values where the registers hold both outputs
   p.wave_tiles = tiles > 1 && c.head_dim <= 128 ? 2 : 1;
   p.tile_groups = (tiles + p.wave_tiles - 1) / p.wave_tiles;
-  const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tile_groups;
-  const int64_t step = 32 * kWaves;
-  // One sequence: as many workgroups as run at once. Several, of lengths that
-  // only the device knows: four times as many, so that short ones even out.
-  const int64_t wanted = ((c.batch == 1 ? 512 : 2048) + groups - 1) / groups;
-  int64_t piece = (max_len + wanted - 1) / wanted;
-  piece = (piece + step - 1) / step * step;
-  if (piece < step) piece = step;
-  p.piece = (int32_t)piece;
-  p.pieces = max_len > 0 ? (int32_t)((max_len + piece - 1) / piece) : 1;
-  p.join = p.pieces > 1 || accumulate;
+  // as many workgroups as run at once, or as there are steps
+  const int64_t groups = (int64_t)c.kv_heads * p.tile_groups;
+  const int64_t at_once = 256 * (c.head_dim > 128 || p.wave_tiles == 2 ? 2 : 3);
+  const int64_t wanted = (at_once + groups - 1) / groups;
+  const int64_t steps = c.batch * ((max_len + kStepTokens - 1) / kStepTokens);
+  p.workgroups = (int32_t)(wanted < steps ? wanted : steps > 0 ? steps : 1);
   return p;
 }
 
@@ -166,16 +167,65 @@ int64_t padded_len(int64_t max_len) { return (max_len + 63) / 64 * 64; }
 
 // floats of the workspace before the scores: statistics (padded to 16 bytes) and outputs
 int64_t stat_floats(const CacheView& c, int32_t heads, const Plan& p) {
-  return ((int64_t)c.batch * heads * p.pieces * 2 + 3) / 4 * 4;
+  return (((int64_t)c.batch + p.workgroups) * heads * 2 + 3) / 4 * 4;
 }
 int64_t part_floats(const CacheView& c, int32_t heads, const Plan& p) {
-  return (int64_t)c.batch * heads * p.pieces * c.head_dim;
+  return ((int64_t)c.batch + p.workgroups) * heads * c.head_dim;
+}
+
+// Steps of sequence i, 0 beyond the batch.
+__device__ __forceinline__ int steps_of(const AttendLaunch& a, int i) {
+  return i < a.c.batch ? (held_tokens(a.lengths, i, a.max_len) + kStepTokens - 1) / kStepTokens : 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+
+// What the sequences add up to, by one wave: all steps, and those before
+// sequence `until`. 64 sequences at a time; the first 64 are handed back.
+__device__ __forceinline__ int all_steps(const AttendLaunch& a, int lane, int until, int* before, int* first) {
+  int total = 0, lower = 0;
+  for (int i0 = 0; i0 < a.c.batch; i0 += 64) {
+    const int v = steps_of(a, i0 + lane);
+    if (i0 == 0) *first = v;
+    total += v;
+    lower += i0 + lane < until ? v : 0;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    total += __shfl_xor(total, off);
+    lower += __shfl_xor(lower, off);
+  }
+  *before = uniform(lower);
+  return uniform(total);
+}
+// The sequence that holds step s < total, and the steps before it; -1 if the
+// lengths no longer add up to that.
+__device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int s, int first, int* before) {
+  int carry = 0;
+  for (int i0 = 0; ; i0 += 64) {
+    const int v = i0 == 0 ? first : steps_of(a, i0 + lane), sum = carry + wave_scan(v, lane);
+    const uint64_t past = __ballot(sum > s);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
+      *before = __builtin_amdgcn_readlane(sum - v, l);
+      return i0 + l;
+    }
+    if (i0 + 64 >= a.c.batch) return -1;
+    carry = __builtin_amdgcn_readlane(sum, 63);
+  }
 }
 
 // NT: blocks of 16 query heads per wave. STREAM: no other workgroup reads the
 // same keys and values.
 template <int CT, int XT, int DP, int NT, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_kernel(AttendLaunch a, Work wk, bool join) {
+__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 2 : DP == 128 ? (NT == 1 ? 3 : 2) : (NT == 1 ? 4 : 3)) void cache_attend_kernel(AttendLaunch a, Work wk) {
   typedef Form<CT, XT, DP> F;
   typedef typename F::C C;
   typedef typename F::X X;
@@ -197,16 +247,25 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Workgroups go to the XCDs in turn: pieces come last, so that the early
-  // ones, which every sequence has, start first, and turn the sequences round,
-  // so that no XCD has the long ones to itself.
-  const int piece = blockIdx.z, b = (blockIdx.y + blockIdx.z) % a.c.batch;
-  const int tile_groups = gridDim.x / a.c.kv_heads;
+  const int u = blockIdx.y, tile_groups = gridDim.x / a.c.kv_heads;
   const int h = blockIdx.x / tile_groups, tile0 = blockIdx.x % tile_groups * NT;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
-  const int n = held_tokens_uniform(a.lengths, b, a.max_len);
-  const int t0 = piece * wk.piece, t1 = min(n, t0 + wk.piece);
-  if (t0 > 0 && t0 >= n) return;                // pieces past the end are not read back
+
+  int before, first64;
+  const int total = all_steps(a, lane, 0, &before, &first64), share = (total + (int)gridDim.y - 1) / (int)gridDim.y;
+  int at = u * share;
+  const int stop = min(total, at + share);
+  if (at >= stop) return;
+  int b = sequence_at(a, lane, at, first64, &before);
+  if (b < 0) return;
+  while (true) {
+  const int n = held_tokens_uniform(a.lengths, b, a.max_len), steps = (n + kStepTokens - 1) / kStepTokens;
+  const int t0 = (at - before) * kStepTokens, t1 = min(n, min(stop - before, steps) * kStepTokens);
+
+  // What only the start and the end of a part need is computed there: kept
+  // in registers through the steps it would cost a wave per SIMD.
+  int own_lane = lane;
+  asm volatile("" : "+v"(own_lane));
 
   // the queries, asked for first (loads come back in order); lanes without a
   // head or column read another's
@@ -214,13 +273,13 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   u32x4 raw[NT][KL][QL];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int head = min((tile0 + nt) * kHeadTile + col, group - 1);
+    const int head = min((tile0 + nt) * kHeadTile + (own_lane & 15), group - 1);
     const char* row = (const char*)a.q + (int64_t)b * a.ldq + ((int64_t)h * group + head) * D * (int)sizeof(X);
 #pragma unroll
     for (int c = 0; c < KL; ++c)
 #pragma unroll
       for (int l = 0; l < QL; ++l)
-        raw[nt][c][l] = *(const u32x4*)(row + min((4 * c + quad) * E, D - E) * (int)sizeof(X) + 16 * l);
+        raw[nt][c][l] = *(const u32x4*)(row + min((4 * c + (own_lane >> 4)) * E, D - E) * (int)sizeof(X) + 16 * l);
   }
 
   // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
@@ -295,12 +354,12 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   float scale[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int head = (tile0 + nt) * kHeadTile + col;
+    const int head = (tile0 + nt) * kHeadTile + (own_lane & 15);
     float x[KL][E];
     float top = 0.0f;
 #pragma unroll
     for (int c = 0; c < KL; ++c) {
-      const bool there = head < group && (4 * c + quad) * E < D;
+      const bool there = head < group && (4 * c + (own_lane >> 4)) * E < D;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         constexpr int PER = 16 / (int)sizeof(X);
@@ -328,7 +387,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
         for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
       }
 #pragma unroll
-      for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][lane] = f[s];
+      for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][own_lane] = f[s];
     }
   }
   lds_barrier();                                // leaves keys and values under way
@@ -460,22 +519,25 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
   if (a.accumulate) release();
 
   // join the waves
+  asm volatile("" : "+v"(own_lane));
+  const int own_col = own_lane & 15, own_quad = own_lane >> 4;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const float all = head_sum(sum[nt]);
-    if (quad == 0) {
-      stat[nt][wave][col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
-      stat[nt][wave][col][1] = all;
+    if (own_quad == 0) {
+      stat[nt][wave][own_col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
+      stat[nt][wave][own_col][1] = all;
     }
   }
   const int chunks = D / 4;
+  const int64_t slot = u + b;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     __syncthreads();
     {
       float common = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stat[nt][w][col][0]);
+      for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stat[nt][w][own_col][0]);
       const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - common);
 #pragma unroll
       for (int v = 0; v < NV; ++v)
@@ -483,15 +545,15 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < EV; j += 4)
-            *(f32x4*)&shared.slab[wave][col][(16 * v + 4 * quad + i) * EV + j] =
+            *(f32x4*)&shared.slab[wave][own_col][(16 * v + 4 * own_quad + i) * EV + j] =
                 f32x4{acc[nt][v][j][i] * f, acc[nt][v][j + 1][i] * f, acc[nt][v][j + 2][i] * f, acc[nt][v][j + 3][i] * f};
     }
     __syncthreads();
     const int g0 = (tile0 + nt) * kHeadTile, live = min(group - g0, kHeadTile);
-    for (int u = tid; u < live * chunks; u += 64 * kWaves) {
-      const int hd = u / chunks, c = u - hd * chunks;
+    for (int k = 64 * wave + own_lane; k < live * chunks; k += 64 * kWaves) {
+      const int hd = k / chunks, c = k - hd * chunks;
       f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-      float common = -INFINITY, total = 0.0f;
+      float common = -INFINITY, weight = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         o += *(const f32x4*)&shared.slab[w][hd][4 * c];
@@ -499,63 +561,73 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) void cache_attend_k
       }
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
-        total += stat[nt][w][hd][1] * (stat[nt][w][hd][0] == -INFINITY ? 0.0f : exp2_fast(stat[nt][w][hd][0] - common));
-      const int64_t row = (int64_t)b * a.heads + h * group + g0 + hd;
-      if (join) {
-        *(f32x4*)(wk.part + (row * wk.pieces + piece) * D + 4 * c) = o;
-        if (c == 0) {
-          wk.stat[2 * (row * wk.pieces + piece)] = common;
-          wk.stat[2 * (row * wk.pieces + piece) + 1] = total;
-        }
-      } else {
-        X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g0 + hd) * D + 4 * c;
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
+        weight += stat[nt][w][hd][1] * (stat[nt][w][hd][0] == -INFINITY ? 0.0f : exp2_fast(stat[nt][w][hd][0] - common));
+      const int64_t row = slot * a.heads + h * group + g0 + hd;
+      *(f32x4*)(wk.part + row * D + 4 * c) = o;
+      if (c == 0) {
+        wk.stat[2 * row] = common;
+        wk.stat[2 * row + 1] = weight;
       }
     }
   }
+
+  // on to the next sequence of this share
+  at = before + steps;
+  if (at >= stop) return;
+  __syncthreads();                              // the outputs are read
+  before = at;
+  do {
+    if (++b >= a.c.batch) return;
+  } while (held_tokens_uniform(a.lengths, b, a.max_len) == 0);
+  }
 }
 
-// Base and sum of a head over its pieces, by one wave.
-__device__ __forceinline__ void head_norm(const float* st, int pieces, int lane, float* common, float* sum) {
+// Base and sum of a head over its parts, `stride` floats apart, by one wave.
+__device__ __forceinline__ void head_norm(const float* st, int64_t stride, int parts, int lane, float* common, float* sum) {
   float m = -INFINITY, l = 0.0f;
-  for (int s = lane; s < pieces; s += 64) m = fmaxf(m, st[2 * s]);
+  for (int s = lane; s < parts; s += 64) m = fmaxf(m, st[s * stride]);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-  for (int s = lane; s < pieces; s += 64) l += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - m));
+  for (int s = lane; s < parts; s += 64)
+    l += st[s * stride + 1] * (st[s * stride] == -INFINITY ? 0.0f : exp2_fast(st[s * stride] - m));
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
   *common = m == -INFINITY ? 0.0f : m;
   *sum = l;
 }
 
-// Joins the pieces. The first `group` workgroups of a key/value head write one
-// query head's output each: rows of 16-byte columns, the pieces dealt out to
-// the rows of threads. The others add the weights of kJoinTokens tokens up,
-// over the heads of the group.
+// Joins the parts. The first `group` workgroups of a key/value head write one
+// query head's output each: rows of 16-byte columns, the parts dealt out to
+// the rows of threads. The others add weights up over the heads of the group,
+// kJoinTokens tokens at a time.
 constexpr int kJoinHeads = 16, kJoinTokens = 4 * 256;
 template <int XT>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk) {
+__global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef typename FloatType<XT>::type X;
   __shared__ f32x4 rows[256];
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.x, b = blockIdx.y, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int n = held_tokens_uniform(a.lengths, b, a.max_len);
-  const int pieces = n == 0 ? 1 : (n + wk.piece - 1) / wk.piece;
+  int before, unused;
+  const int total = all_steps(a, lane, b, &before, &unused), share = max((total + workgroups - 1) / workgroups, 1);
+  const int steps = (n + kStepTokens - 1) / kStepTokens, u0 = before / share;
+  const int parts = steps == 0 ? 0 : (before + steps - 1) / share - u0 + 1;
+  const int64_t head0 = (int64_t)(u0 + b) * a.heads + h * group;      // of the first part
+  const int64_t stride = 2 * (int64_t)a.heads;
   if ((int)blockIdx.z < group) {
-    const int64_t row = (int64_t)b * a.heads + h * group + blockIdx.z;
-    const float* st = wk.stat + 2 * row * wk.pieces;
+    const int64_t row = head0 + blockIdx.z;
+    const float* st = wk.stat + 2 * row;
     float common, sum;
-    head_norm(st, pieces, lane, &common, &sum);   // every wave for itself
+    head_norm(st, stride, parts, lane, &common, &sum);   // every wave for itself
     const int cols = D / 4, at_once = 256 / cols, c = tid % cols, s0 = tid / cols;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     if (s0 < at_once) {
-      const float* part = wk.part + row * wk.pieces * D + 4 * c;
+      const float* part = wk.part + row * D + 4 * c;
 #pragma unroll 4
-      for (int s = s0; s < pieces; s += at_once)
-        o += *(const f32x4*)(part + (int64_t)s * D) * (st[2 * s] == -INFINITY ? 0.0f : exp2_fast(st[2 * s] - common));
+      for (int s = s0; s < parts; s += at_once)
+        o += *(const f32x4*)(part + (int64_t)s * a.heads * D) *
+             (st[s * stride] == -INFINITY ? 0.0f : exp2_fast(st[s * stride] - common));
     }
     rows[tid] = o;
     __syncthreads();
@@ -567,18 +639,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
     for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
     return;
   }
-  const int t0 = ((int)blockIdx.z - group) * kJoinTokens;
-  if (t0 >= n) return;
+  for (int t0 = ((int)blockIdx.z - group) * kJoinTokens; t0 < n; t0 += ((int)gridDim.z - group) * kJoinTokens) {
   const int t = t0 + 4 * tid;                     // four tokens of one page
   const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
   f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
     const int count = min(group - g0, kJoinHeads);
-    const int64_t row0 = (int64_t)b * a.heads + h * group + g0;
     __syncthreads();
     for (int g = wave; g < count; g += 4) {
       float common, sum;
-      head_norm(wk.stat + 2 * (row0 + g) * wk.pieces, pieces, lane, &common, &sum);
+      head_norm(wk.stat + 2 * (head0 + g0 + g), stride, parts, lane, &common, &sum);
       if (lane == 0) {
         norm[g][0] = common;
         norm[g][1] = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -595,7 +665,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
     }
   }
   const int page = t < n ? page_of(a.c, b, t) : -1;
-  if (page < 0) return;
+  if (page < 0) continue;
   float* dst = a.c.weights + row_index(a.c, page, h, t);
   if (t + 4 <= n) {
     *(f32x4_any*)dst += w;
@@ -605,47 +675,49 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
       if (t + i < n) dst[i] += w[i];
   }
 }
+}
 
 template <int CT, int XT, int DP>
 void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
-  const dim3 grid(a.c.kv_heads * p.tile_groups, a.c.batch, p.pieces), block(64 * kWaves);
+  const dim3 grid(a.c.kv_heads * p.tile_groups, p.workgroups), block(64 * kWaves);
   if constexpr (DP < 256) {
     if (p.wave_tiles == 2) {
-      if (p.tile_groups == 1) cache_attend_kernel<CT, XT, DP, 2, true><<<grid, block, 0, s>>>(a, w, p.join);
-      else cache_attend_kernel<CT, XT, DP, 2, false><<<grid, block, 0, s>>>(a, w, p.join);
+      if (p.tile_groups == 1) cache_attend_kernel<CT, XT, DP, 2, true><<<grid, block, 0, s>>>(a, w);
+      else cache_attend_kernel<CT, XT, DP, 2, false><<<grid, block, 0, s>>>(a, w);
       return;
     }
   } else if (p.tile_groups > 1) {
-    cache_attend_kernel<CT, XT, DP, 1, false><<<grid, block, 0, s>>>(a, w, p.join);
+    cache_attend_kernel<CT, XT, DP, 1, false><<<grid, block, 0, s>>>(a, w);
     return;
   }
-  cache_attend_kernel<CT, XT, DP, 1, true><<<grid, block, 0, s>>>(a, w, p.join);
+  cache_attend_kernel<CT, XT, DP, 1, true><<<grid, block, 0, s>>>(a, w);
 }
 
 template <int CT, int XT>
 hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
-  const Plan p = plan_of(a.c, a.heads, a.max_len, a.accumulate);
-  Work w = {nullptr, nullptr, nullptr, padded_len(a.max_len), p.pieces, p.piece};
-  if (p.join) {
-    w.stat = (float*)a.workspace;
-    w.part = w.stat + stat_floats(a.c, a.heads, p);
-    w.scores = w.part + part_floats(a.c, a.heads, p);
-  }
+  const Plan p = plan_of(a.c, a.heads, a.max_len);
+  Work w;
+  w.stat = (float*)a.workspace;
+  w.part = w.stat + stat_floats(a.c, a.heads, p);
+  w.scores = w.part + part_floats(a.c, a.heads, p);
+  w.row = padded_len(a.max_len);
   if (a.c.head_dim <= 64) launch_tiles<CT, XT, 64>(a, w, p, s);
   else if (a.c.head_dim <= 128) launch_tiles<CT, XT, 128>(a, w, p, s);
   else launch_tiles<CT, XT, 256>(a, w, p, s);
-  if (p.join) {
-    const int64_t ranges = a.accumulate ? (a.max_len + kJoinTokens - 1) / kJoinTokens : 0;
-    cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, (unsigned)(a.heads / a.c.kv_heads + ranges)), 256, 0, s>>>(a, w);
+  // weights: a workgroup per range of tokens, fewer where the heads are many
+  int64_t ranges = 0;
+  if (a.accumulate) {
+    const int64_t all = (a.max_len + kJoinTokens - 1) / kJoinTokens, most = 4096 / ((int64_t)a.c.kv_heads * a.c.batch) + 1;
+    ranges = all < most ? all : most;
   }
+  cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, (unsigned)(a.heads / a.c.kv_heads + ranges)), 256, 0, s>>>(a, w, p.workgroups);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t cache_attend_workspace(const CacheView& c, int32_t heads, int64_t max_len, int32_t accumulate) {
-  const Plan p = plan_of(c, heads, max_len, accumulate);
-  if (!p.join) return 0;
+  const Plan p = plan_of(c, heads, max_len);
   const int64_t scores = accumulate ? (int64_t)c.batch * heads * padded_len(max_len) : 0;
   return 4 * (stat_floats(c, heads, p) + part_floats(c, heads, p) + scores);
 }

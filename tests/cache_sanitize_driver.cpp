@@ -169,6 +169,7 @@ int main() {
   REFUSE(Attend, UNSUPPORTED, t.dtype = MOSAIC_F16);
   REFUSE(Attend, INVALID, t.dtype = 9);
   REFUSE(Attend, INVALID, t.max_len = -1);
+  REFUSE(Attend, UNSUPPORTED, t.c.batch = 65535; t.c.max_blocks = t.c.ldt = 1 << 26; t.max_len = INT64_MAX);
   REFUSE(Attend, INVALID, t.scale = NAN);
   REFUSE(Attend, INVALID, t.scale = 3e38f);
   REFUSE(Attend, INVALID, t.q = nullptr);
