@@ -12,6 +12,8 @@
 namespace mosaic {
 namespace {
 
+constexpr int kFewRows = 256;     // no more than one workgroup per compute unit
+
 // How the elements of a pair lie. A thread works on V consecutive elements
 // (16 bytes of the row).
 enum RotaryMode {
@@ -75,6 +77,30 @@ __device__ __forceinline__ void store_chunk(const AppendLaunch& a, char* q, int6
   }
 }
 
+// A thread's piece of the row: V elements of a head, and the V that they are
+// paired with P further on (ROT_HALVES).
+template <int XT, int MODE> struct Unit {
+  typedef typename FloatType<XT>::type X;
+  static constexpr int V = 16 / sizeof(X);
+  int head, e0;                                  // of the row; first element in the head
+  bool turned, pair;                             // rotated head; with a partner chunk
+  Chunk<X, V> a, b;
+
+  __device__ __forceinline__ void load(const AppendLaunch& l, const char* x, int u) {
+    const int D = l.c.head_dim, P = l.rot.pairs, chunks = D / V, pc = MODE == ROT_HALVES ? P / V : 0;
+    const int turned_heads = l.heads + l.c.kv_heads, per_turned = chunks - pc, first = turned_heads * per_turned;
+    turned = u < first;
+    const int w = turned ? u : u - first, per = turned ? per_turned : chunks;
+    const int q = w / per, r = w - q * per;
+    head = q + (turned ? 0 : turned_heads);
+    pair = turned && MODE == ROT_HALVES && r < pc;
+    e0 = V * (MODE == ROT_HALVES && turned && r >= pc ? r + pc : r);
+    const char* at = x + ((int64_t)head * D + e0) * sizeof(X);
+    a = *(const Chunk<X, V>*)at;
+    if (pair) b = *(const Chunk<X, V>*)(at + P * sizeof(X));
+  }
+};
+
 template <int XT, int CT, int MODE>
 __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
   typedef typename FloatType<XT>::type X;
@@ -82,16 +108,22 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
   __shared__ float turn[256];                    // cosines of the P pairs, then sines
   const int64_t t = blockIdx.x;
   const int threads = blockDim.x, tid = threadIdx.x;
+  const char* x = (const char*)a.x + t * a.ldx;
+  char* q = (char*)a.q + t * a.ldq;
+  const int P = a.rot.pairs, D = a.c.head_dim;
+  const int units = (a.heads + a.c.kv_heads) * (D / V - (MODE == ROT_HALVES ? P / V : 0)) + a.c.kv_heads * (D / V);
+  Unit<XT, MODE> unit;
+  if (tid < units) unit.load(a, x, tid);         // under way while the token's place is found
+
   const int b = a.starts == nullptr ? (int)t : sequence_of(a.starts, a.c.batch, t);
   const int32_t i = a.starts == nullptr ? 0 : (int32_t)(t - a.starts[b]);
   const int64_t slots = (int64_t)a.c.max_blocks << a.c.log2_page;
-  const int64_t slot = (int64_t)held_tokens(a.state, b, slots) + i;
+  const int64_t slot = (int64_t)__builtin_amdgcn_readfirstlane(held_tokens(a.state, b, slots)) + i;
   const int32_t number = (int32_t)((uint32_t)a.state[a.c.batch + b] + (uint32_t)i);
-  const int32_t page = slot >= 0 && slot < slots ? page_of(a.c, b, slot) : -1;
+  const int32_t page = slot >= 0 && slot < slots ? page_of_uniform(a.c, b, (int32_t)slot) : -1;
   const bool kept = page >= 0;
   const int64_t kv_off = kept ? row_offset(a.c, page, 0, slot) : 0;
 
-  const int P = a.rot.pairs;
   for (int j = tid; j < P; j += threads) {
     const int axis = (j >= a.rot.ends[0]) + (j >= a.rot.ends[1]) + (j >= a.rot.ends[2]);
     int64_t p = a.rot.positions != nullptr ? a.rot.positions[axis * a.rot.ldp + t] : number;
@@ -112,42 +144,30 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
     if (a.c.order != nullptr) a.c.order[r] = number;
   }
 
-  const char* x = (const char*)a.x + t * a.ldx;
-  char* q = (char*)a.q + t * a.ldq;
-  const int D = a.c.head_dim, chunks = D / V, pc = MODE == ROT_HALVES ? P / V : 0;
-  const int turned_heads = a.heads + a.c.kv_heads;
-  const int per_turned = chunks - pc;            // units of a rotated head; a value head has `chunks`
-  const int units = turned_heads * per_turned + a.c.kv_heads * chunks;
   for (int u = tid; u < units; u += threads) {
-    const bool turned = u < turned_heads * per_turned;
-    const int w = turned ? u : u - turned_heads * per_turned;
-    const int per = turned ? per_turned : chunks;
-    const int head = w / per + (turned ? 0 : turned_heads), r = w - (w / per) * per;
-    const char* xh = x + (int64_t)head * D * sizeof(X);
-    const int e0 = V * (MODE == ROT_HALVES && turned && r >= pc ? r + pc : r);
+    if (u != tid) unit.load(a, x, u);
+    const int head = unit.head, e0 = unit.e0;
+    const bool turned = unit.turned;
     float v[V], y[V];
-    {
-      const Chunk<X, V> c = *(const Chunk<X, V>*)(xh + e0 * sizeof(X));
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = y[k] = (float)c.e[k];
-    }
-    if (turned && MODE == ROT_HALVES && r < pc) {
-      const Chunk<X, V> c = *(const Chunk<X, V>*)(xh + (e0 + P) * sizeof(X));
+    for (int k = 0; k < V; ++k) v[k] = y[k] = (float)unit.a.e[k];
+    if (MODE == ROT_HALVES && unit.pair) {
       float z[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float o = (float)c.e[k], cs = turn[e0 + k], sn = turn[P + e0 + k];
+        const float o = (float)unit.b.e[k], cs = turn[e0 + k], sn = turn[P + e0 + k];
         y[k] = v[k] * cs - o * sn;
         z[k] = o * cs + v[k] * sn;
       }
       store_chunk<XT, CT, V>(a, q, kv_off, kept, head, e0 + P, z);
     } else if (turned && MODE == ROT_HALVES_RAGGED) {
+      const X* xh = (const X*)x + (int64_t)head * D;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const int e = e0 + k;
         if (e < 2 * P) {
           const int j = e < P ? e : e - P;
-          const float o = (float)((const X*)xh)[e < P ? e + P : e - P];
+          const float o = (float)xh[e < P ? e + P : e - P];
           y[k] = e < P ? v[k] * turn[j] - o * turn[P + j] : v[k] * turn[j] + o * turn[P + j];
         }
       }
@@ -168,7 +188,8 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
 template <int XT, int CT>
 void launch_mode(const AppendLaunch& a, hipStream_t s) {
   constexpr int V = XT == MOSAIC_F32 ? 4 : 8;
-  const dim3 grid((unsigned)a.rows), block(256);
+  // few tokens: a thread per piece of a row, so that all of it is asked for at once
+  const dim3 grid((unsigned)a.rows), block(a.rows <= kFewRows ? 1024 : 256);
   if (a.rot.pairs == 0 || a.rot.interleaved) cache_append_kernel<XT, CT, ROT_NEIGHBOURS><<<grid, block, 0, s>>>(a);
   else if (a.rot.pairs % V == 0) cache_append_kernel<XT, CT, ROT_HALVES><<<grid, block, 0, s>>>(a);
   else cache_append_kernel<XT, CT, ROT_HALVES_RAGGED><<<grid, block, 0, s>>>(a);

@@ -596,18 +596,19 @@ __device__ __forceinline__ void head_norm(const float* st, int64_t stride, int p
   *sum = l;
 }
 
-// Joins the parts. The first `group` workgroups of a key/value head write one
-// query head's output each: rows of 16-byte columns, the parts dealt out to
-// the rows of threads. The others add weights up over the heads of the group,
-// kJoinTokens tokens at a time.
+// Joins the parts. The first `out_groups` workgroups of a key/value head write
+// the outputs of `out_heads` query heads each: rows of 16-byte columns, a
+// head's parts dealt out to its share of the rows of threads. The others add
+// weights up over the heads of the group, kJoinTokens tokens at a time.
 constexpr int kJoinHeads = 16, kJoinTokens = 4 * 256;
 template <int XT>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
+__global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk, int32_t workgroups, int32_t out_heads) {
   typedef typename FloatType<XT>::type X;
   __shared__ f32x4 rows[256];
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.x, b = blockIdx.y, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
+  const int out_groups = (group + out_heads - 1) / out_heads;
   const int n = held_tokens_uniform(a.lengths, b, a.max_len);
   int before, unused;
   const int total = all_steps(a, lane, b, &before, &unused), share = max((total + workgroups - 1) / workgroups, 1);
@@ -615,37 +616,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
   const int parts = steps == 0 ? 0 : (before + steps - 1) / share - u0 + 1;
   const int64_t head0 = (int64_t)(u0 + b) * a.heads + h * group;      // of the first part
   const int64_t stride = 2 * (int64_t)a.heads;
-  if ((int)blockIdx.z < group) {
-    const int64_t row = head0 + blockIdx.z;
-    const float* st = wk.stat + 2 * row;
-    float common, sum;
-    head_norm(st, stride, parts, lane, &common, &sum);   // every wave for itself
-    const int cols = D / 4, at_once = 256 / cols, c = tid % cols, s0 = tid / cols;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (s0 < at_once) {
-      const float* part = wk.part + row * D + 4 * c;
-#pragma unroll 4
-      for (int s = s0; s < parts; s += at_once)
-        o += *(const f32x4*)(part + (int64_t)s * a.heads * D) *
-             (st[s * stride] == -INFINITY ? 0.0f : exp2_fast(st[s * stride] - common));
-    }
-    rows[tid] = o;
-    __syncthreads();
-    if (tid >= cols) return;
-    for (int s = 1; s < at_once; ++s) o += rows[s * cols + tid];
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + blockIdx.z) * D + 4 * tid;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
-    return;
-  }
-  for (int t0 = ((int)blockIdx.z - group) * kJoinTokens; t0 < n; t0 += ((int)gridDim.z - group) * kJoinTokens) {
-  const int t = t0 + 4 * tid;                     // four tokens of one page
-  const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
-  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
-    const int count = min(group - g0, kJoinHeads);
-    __syncthreads();
+  // base and 1 / sum of heads g0 .. g0 + count - 1 of the group
+  auto norms = [&](int g0, int count) {
     for (int g = wave; g < count; g += 4) {
       float common, sum;
       head_norm(wk.stat + 2 * (head0 + g0 + g), stride, parts, lane, &common, &sum);
@@ -655,6 +627,38 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
       }
     }
     __syncthreads();
+  };
+  if ((int)blockIdx.z < out_groups) {
+    const int g0 = blockIdx.z * out_heads, count = min(group - g0, out_heads);
+    norms(g0, count);
+    const int cols = D / 4, each = 256 / cols / out_heads;            // rows of a head
+    const int c = tid % cols, r = tid / cols, hd = r / each, s0 = r - hd * each;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (hd < count) {
+      const float* st = wk.stat + 2 * (head0 + g0 + hd);
+      const float* part = wk.part + (head0 + g0 + hd) * D + 4 * c;
+#pragma unroll 4
+      for (int s = s0; s < parts; s += each)
+        o += *(const f32x4*)(part + (int64_t)s * a.heads * D) *
+             (st[s * stride] == -INFINITY ? 0.0f : exp2_fast(st[s * stride] - norm[hd][0]));
+    }
+    rows[tid] = o;
+    __syncthreads();
+    if (hd >= count || s0 > 0) return;
+    for (int s = 1; s < each; ++s) o += rows[tid + s * cols];
+    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g0 + hd) * D + 4 * c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * norm[hd][1]);
+    return;
+  }
+  for (int t0 = ((int)blockIdx.z - out_groups) * kJoinTokens; t0 < n; t0 += ((int)gridDim.z - out_groups) * kJoinTokens) {
+  const int t = t0 + 4 * tid;                     // four tokens of one page
+  const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
+  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
+    const int count = min(group - g0, kJoinHeads);
+    __syncthreads();
+    norms(g0, count);
     if (t < n) {
 #pragma unroll 8
       for (int g = 0; g < count; ++g) {
@@ -710,7 +714,12 @@ hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
     const int64_t all = (a.max_len + kJoinTokens - 1) / kJoinTokens, most = 4096 / ((int64_t)a.c.kv_heads * a.c.batch) + 1;
     ranges = all < most ? all : most;
   }
-  cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, (unsigned)(a.heads / a.c.kv_heads + ranges)), 256, 0, s>>>(a, w, p.workgroups);
+  // several heads per workgroup where there are many and a sequence has few parts
+  const int32_t group = a.heads / a.c.kv_heads, rows = 256 / (a.c.head_dim / 4);
+  int32_t out_heads = (int64_t)a.c.kv_heads * a.c.batch < 64 ? 1 : rows < 4 ? rows : 4;
+  if (out_heads > group) out_heads = group;
+  const unsigned z = (unsigned)((group + out_heads - 1) / out_heads + ranges);
+  cache_join_kernel<XT><<<dim3(a.c.kv_heads, a.c.batch, z), 256, 0, s>>>(a, w, p.workgroups, out_heads);
   return hipGetLastError();
 }
 
