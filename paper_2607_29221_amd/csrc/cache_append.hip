@@ -7,12 +7,17 @@
 // cosines and sines into LDS once and every head reads them from there, so a
 // row of q|k|v is read once and every output written once.
 #include "cache.h"
+#include "device_common.h"
 #include "dispatch.h"
 
 namespace mosaic {
 namespace {
 
 constexpr int kFewRows = 256;     // no more than one workgroup per compute unit
+// Rows that the 32 MiB of second-level cache cannot hold pass by it (168 MB of
+// q|k|v: 61 us, 68 us through it); fewer are left there for the attention that
+// comes next.
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 
 // How the elements of a pair lie. A thread works on V consecutive elements
 // (16 bytes of the row).
@@ -54,8 +59,18 @@ __global__ __launch_bounds__(256) void cache_advance_kernel(AppendLaunch a) {
 
 template <class T, int V> struct alignas(sizeof(T) * V) Chunk { T e[V]; };
 
+// STREAM: past the caches.
+template <bool STREAM, class T> __device__ __forceinline__ T load_piece(const char* p) {
+  if constexpr (STREAM) return __builtin_bit_cast(T, __builtin_nontemporal_load((const u32x4*)p));
+  else return *(const T*)p;
+}
+template <bool STREAM, class T> __device__ __forceinline__ void store_piece(char* p, T v) {
+  if constexpr (STREAM && sizeof(T) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+  else *(T*)p = v;
+}
+
 // Where a chunk of a head goes: q_out, or the head's row of k or v.
-template <int XT, int CT, int V>
+template <int XT, int CT, bool STREAM, int V>
 __device__ __forceinline__ void store_chunk(const AppendLaunch& a, char* q, int64_t kv_off, bool kept, int head,
                                             int e0, const float* y) {
   typedef typename FloatType<XT>::type X;
@@ -65,7 +80,7 @@ __device__ __forceinline__ void store_chunk(const AppendLaunch& a, char* q, int6
     Chunk<X, V> o;
 #pragma unroll
     for (int i = 0; i < V; ++i) o.e[i] = (X)y[i];
-    *(Chunk<X, V>*)(q + ((int64_t)head * D + e0) * sizeof(X)) = o;
+    store_piece<STREAM>(q + ((int64_t)head * D + e0) * sizeof(X), o);
   } else if (kept) {
     const int h = head - a.heads;
     const bool value = h >= a.c.kv_heads;
@@ -73,13 +88,13 @@ __device__ __forceinline__ void store_chunk(const AppendLaunch& a, char* q, int6
 #pragma unroll
     for (int i = 0; i < V; ++i) o.e[i] = (C)y[i];
     char* base = (value ? a.c.v : a.c.k) + kv_off + (value ? h - a.c.kv_heads : h) * a.c.head_stride;
-    *(Chunk<C, V>*)(base + e0 * sizeof(C)) = o;
+    store_piece<STREAM>(base + e0 * sizeof(C), o);
   }
 }
 
 // A thread's piece of the row: V elements of a head, and the V that they are
 // paired with P further on (ROT_HALVES).
-template <int XT, int MODE> struct Unit {
+template <int XT, int MODE, bool STREAM> struct Unit {
   typedef typename FloatType<XT>::type X;
   static constexpr int V = 16 / sizeof(X);
   int head, e0;                                  // of the row; first element in the head
@@ -96,12 +111,12 @@ template <int XT, int MODE> struct Unit {
     pair = turned && MODE == ROT_HALVES && r < pc;
     e0 = V * (MODE == ROT_HALVES && turned && r >= pc ? r + pc : r);
     const char* at = x + ((int64_t)head * D + e0) * sizeof(X);
-    a = *(const Chunk<X, V>*)at;
-    if (pair) b = *(const Chunk<X, V>*)(at + P * sizeof(X));
+    a = load_piece<STREAM, Chunk<X, V>>(at);
+    if (pair) b = load_piece<STREAM, Chunk<X, V>>(at + P * sizeof(X));
   }
 };
 
-template <int XT, int CT, int MODE>
+template <int XT, int CT, int MODE, bool STREAM>
 __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
   typedef typename FloatType<XT>::type X;
   constexpr int V = 16 / sizeof(X);
@@ -112,7 +127,7 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
   char* q = (char*)a.q + t * a.ldq;
   const int P = a.rot.pairs, D = a.c.head_dim;
   const int units = (a.heads + a.c.kv_heads) * (D / V - (MODE == ROT_HALVES ? P / V : 0)) + a.c.kv_heads * (D / V);
-  Unit<XT, MODE> unit;
+  Unit<XT, MODE, STREAM> unit;
   if (tid < units) unit.load(a, x, tid);         // under way while the token's place is found
 
   const int b = a.starts == nullptr ? (int)t : sequence_of(a.starts, a.c.batch, t);
@@ -159,7 +174,7 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
         y[k] = v[k] * cs - o * sn;
         z[k] = o * cs + v[k] * sn;
       }
-      store_chunk<XT, CT, V>(a, q, kv_off, kept, head, e0 + P, z);
+      store_chunk<XT, CT, STREAM, V>(a, q, kv_off, kept, head, e0 + P, z);
     } else if (turned && MODE == ROT_HALVES_RAGGED) {
       const X* xh = (const X*)x + (int64_t)head * D;
 #pragma unroll
@@ -181,29 +196,36 @@ __global__ __launch_bounds__(1024) void cache_append_kernel(AppendLaunch a) {
         }
       }
     }
-    store_chunk<XT, CT, V>(a, q, kv_off, kept, head, e0, y);
+    store_chunk<XT, CT, STREAM, V>(a, q, kv_off, kept, head, e0, y);
   }
 }
 
-template <int XT, int CT>
+template <int XT, int CT, bool STREAM>
 void launch_mode(const AppendLaunch& a, hipStream_t s) {
   constexpr int V = XT == MOSAIC_F32 ? 4 : 8;
   // few tokens: a thread per piece of a row, so that all of it is asked for at once
   const dim3 grid((unsigned)a.rows), block(a.rows <= kFewRows ? 1024 : 256);
-  if (a.rot.pairs == 0 || a.rot.interleaved) cache_append_kernel<XT, CT, ROT_NEIGHBOURS><<<grid, block, 0, s>>>(a);
-  else if (a.rot.pairs % V == 0) cache_append_kernel<XT, CT, ROT_HALVES><<<grid, block, 0, s>>>(a);
-  else cache_append_kernel<XT, CT, ROT_HALVES_RAGGED><<<grid, block, 0, s>>>(a);
+  if (a.rot.pairs == 0 || a.rot.interleaved) cache_append_kernel<XT, CT, ROT_NEIGHBOURS, STREAM><<<grid, block, 0, s>>>(a);
+  else if (a.rot.pairs % V == 0) cache_append_kernel<XT, CT, ROT_HALVES, STREAM><<<grid, block, 0, s>>>(a);
+  else cache_append_kernel<XT, CT, ROT_HALVES_RAGGED, STREAM><<<grid, block, 0, s>>>(a);
+}
+
+template <int XT, int CT>
+void launch_types(const AppendLaunch& a, hipStream_t s) {
+  const int64_t row = (a.heads + 2 * (int64_t)a.c.kv_heads) * a.c.head_dim * (XT == MOSAIC_F32 ? 4 : 2);
+  if (a.rows * row >= kStreamBytes) launch_mode<XT, CT, true>(a, s);
+  else launch_mode<XT, CT, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_cache_append(const AppendLaunch& a, hipStream_t s) {
   if (a.rows > 0) {
-    if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_F32) launch_mode<MOSAIC_F32, MOSAIC_F32>(a, s);
-    else if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_BF16) launch_mode<MOSAIC_F32, MOSAIC_BF16>(a, s);
-    else if (a.x_dtype == MOSAIC_F32) launch_mode<MOSAIC_F32, MOSAIC_F16>(a, s);
-    else if (a.c.dtype == MOSAIC_BF16) launch_mode<MOSAIC_BF16, MOSAIC_BF16>(a, s);
-    else launch_mode<MOSAIC_F16, MOSAIC_F16>(a, s);
+    if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_F32) launch_types<MOSAIC_F32, MOSAIC_F32>(a, s);
+    else if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_BF16) launch_types<MOSAIC_F32, MOSAIC_BF16>(a, s);
+    else if (a.x_dtype == MOSAIC_F32) launch_types<MOSAIC_F32, MOSAIC_F16>(a, s);
+    else if (a.c.dtype == MOSAIC_BF16) launch_types<MOSAIC_BF16, MOSAIC_BF16>(a, s);
+    else launch_types<MOSAIC_F16, MOSAIC_F16>(a, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

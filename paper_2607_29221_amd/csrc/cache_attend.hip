@@ -179,55 +179,66 @@ int64_t part_floats(const CacheView& c, int32_t heads, const Plan& p) {
 __device__ __forceinline__ int steps_of(const AttendLaunch& a, int i) {
   return i < a.c.batch ? (held_tokens(a.lengths, i, a.max_len) + kStepTokens - 1) / kStepTokens : 0;
 }
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int wave_scan(int v, int lane) {
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int o = __shfl_up(v, off);
-    if (lane >= off) v += o;
-  }
+// Sums of v over the lanes up to this one: within rows of 16 by shifts, then
+// across rows.
+template <int CTRL, int ROWS> __device__ __forceinline__ int lanes_before(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v += lanes_before<0x111, 0xF>(v);
+  v += lanes_before<0x112, 0xF>(v);
+  v += lanes_before<0x114, 0xF>(v);
+  v += lanes_before<0x118, 0xF>(v);
+  v += lanes_before<0x142, 0xA>(v);       // a row's last lane to the next row (rows 1 and 3)
+  v += lanes_before<0x143, 0xC>(v);       // lane 31 to rows 2 and 3
   return v;
 }
 
-// What the sequences add up to, by one wave: all steps, and those before
-// sequence `until`. 64 sequences at a time; the first 64 are handed back.
-__device__ __forceinline__ int all_steps(const AttendLaunch& a, int lane, int until, int* before, int* first) {
-  int total = 0, lower = 0;
-  for (int i0 = 0; i0 < a.c.batch; i0 += 64) {
-    const int v = steps_of(a, i0 + lane);
-    if (i0 == 0) *first = v;
-    total += v;
-    lower += i0 + lane < until ? v : 0;
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    total += __shfl_xor(total, off);
-    lower += __shfl_xor(lower, off);
-  }
-  *before = uniform(lower);
-  return uniform(total);
+// Steps of the first 64 sequences, a lane each: its own, and all up to it.
+struct FirstSteps {
+  int own, upto;
+};
+// Steps of all sequences, by one wave.
+__device__ __forceinline__ int all_steps(const AttendLaunch& a, int lane, FirstSteps* first) {
+  first->own = steps_of(a, lane);
+  first->upto = wave_scan(first->own);
+  int total = __builtin_amdgcn_readlane(first->upto, 63);
+  for (int i0 = 64; i0 < a.c.batch; i0 += 64) total += __builtin_amdgcn_readlane(wave_scan(steps_of(a, i0 + lane)), 63);
+  return total;
 }
-// The sequence that holds step s < total, and the steps before it; -1 if the
-// lengths no longer add up to that.
-__device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int s, int first, int* before) {
-  int carry = 0;
-  for (int i0 = 0; ; i0 += 64) {
-    const int v = i0 == 0 ? first : steps_of(a, i0 + lane), sum = carry + wave_scan(v, lane);
-    const uint64_t past = __ballot(sum > s);
+// Steps of the sequences before b.
+__device__ __forceinline__ int steps_before(const AttendLaunch& a, int lane, int b, const FirstSteps& first) {
+  if (b < 64) return __builtin_amdgcn_readlane(first.upto - first.own, b);
+  int carry = __builtin_amdgcn_readlane(first.upto, 63);
+  for (int i0 = 64; ; i0 += 64) {
+    const int own = steps_of(a, i0 + lane), upto = wave_scan(own);
+    if (b < i0 + 64) return carry + __builtin_amdgcn_readlane(upto - own, b - i0);
+    carry += __builtin_amdgcn_readlane(upto, 63);
+  }
+}
+// The sequence that holds step s, and the steps before it; -1 if the lengths
+// do not add up to that.
+__device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int s, const FirstSteps& first, int* before) {
+  int carry = 0, own = first.own, upto = first.upto;
+  for (int i0 = 0; ; ) {
+    const uint64_t past = __ballot(carry + upto > s);
     if (past != 0) {
       const int l = __builtin_ctzll(past);
-      *before = __builtin_amdgcn_readlane(sum - v, l);
+      *before = carry + __builtin_amdgcn_readlane(upto - own, l);
       return i0 + l;
     }
-    if (i0 + 64 >= a.c.batch) return -1;
-    carry = __builtin_amdgcn_readlane(sum, 63);
+    i0 += 64;
+    if (i0 >= a.c.batch) return -1;
+    carry += __builtin_amdgcn_readlane(upto, 63);
+    own = steps_of(a, i0 + lane);
+    upto = wave_scan(own);
   }
 }
 
 // NT: blocks of 16 query heads per wave. STREAM: no other workgroup reads the
 // same keys and values.
 template <int CT, int XT, int DP, int NT, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 2 : DP == 128 ? (NT == 1 ? 3 : 2) : (NT == 1 ? 4 : 3)) void cache_attend_kernel(AttendLaunch a, Work wk) {
+__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ? 3 : 2) : (NT == 1 ? 4 : 3)) void cache_attend_kernel(AttendLaunch a, Work wk) {
   typedef Form<CT, XT, DP> F;
   typedef typename F::C C;
   typedef typename F::X X;
@@ -253,8 +264,9 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 2 : DP == 128 ? (NT == 1 ?
   const int h = blockIdx.x / tile_groups, tile0 = blockIdx.x % tile_groups * NT;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
 
-  int before, first64;
-  const int total = all_steps(a, lane, 0, &before, &first64), share = (total + (int)gridDim.y - 1) / (int)gridDim.y;
+  int before;
+  FirstSteps first64;
+  const int total = all_steps(a, lane, &first64), share = (total + (int)gridDim.y - 1) / (int)gridDim.y;
   int at = u * share;
   const int stop = min(total, at + share);
   if (at >= stop) return;
@@ -607,17 +619,54 @@ template <int XT>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk, int32_t workgroups, int32_t out_heads) {
   typedef typename FloatType<XT>::type X;
   __shared__ f32x4 rows[256];
+  __shared__ float row_stat[129][2];              // at most 128 rows of threads, and the threads over
   __shared__ float norm[kJoinHeads][2];           // common base, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.x, b = blockIdx.y, group = a.heads / a.c.kv_heads, D = a.c.head_dim;
   const int out_groups = (group + out_heads - 1) / out_heads;
   const int n = held_tokens_uniform(a.lengths, b, a.max_len);
-  int before, unused;
-  const int total = all_steps(a, lane, b, &before, &unused), share = max((total + workgroups - 1) / workgroups, 1);
+  FirstSteps first64;
+  const int total = all_steps(a, lane, &first64), share = max((total + workgroups - 1) / workgroups, 1);
+  const int before = steps_before(a, lane, b, first64);
   const int steps = (n + kStepTokens - 1) / kStepTokens, u0 = before / share;
   const int parts = steps == 0 ? 0 : (before + steps - 1) / share - u0 + 1;
   const int64_t head0 = (int64_t)(u0 + b) * a.heads + h * group;      // of the first part
   const int64_t stride = 2 * (int64_t)a.heads;
+  if ((int)blockIdx.z < out_groups) {
+    const int g0 = blockIdx.z * out_heads, count = min(group - g0, out_heads);
+    const int cols = D / 4, each = 256 / cols / out_heads;            // rows of a head
+    const int c = tid % cols, r = tid / cols, hd = r / each, s0 = r - hd * each;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    float base = -INFINITY, sum = 0.0f;
+    // adds what has base m and sum l
+    auto add = [&](f32x4 x, float m, float l) {
+      const float now = fmaxf(base, m);
+      const float f = base == -INFINITY ? 0.0f : exp2_fast(base - now), e = m == -INFINITY ? 0.0f : exp2_fast(m - now);
+      o = o * f + x * e;
+      sum = sum * f + l * e;
+      base = now;
+    };
+    if (hd < count) {
+      const float* st = wk.stat + 2 * (head0 + g0 + hd);
+      const float* part = wk.part + (head0 + g0 + hd) * D + 4 * c;
+#pragma unroll 4
+      for (int s = s0; s < parts; s += each)
+        add(*(const f32x4*)(part + (int64_t)s * a.heads * D), st[s * stride], st[s * stride + 1]);
+    }
+    rows[tid] = o;
+    if (c == 0) {
+      row_stat[r][0] = base;
+      row_stat[r][1] = sum;
+    }
+    __syncthreads();
+    if (hd >= count || s0 > 0) return;
+    for (int s = 1; s < each; ++s) add(rows[tid + s * cols], row_stat[r + s][0], row_stat[r + s][1]);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g0 + hd) * D + 4 * c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * inv);
+    return;
+  }
   // base and 1 / sum of heads g0 .. g0 + count - 1 of the group
   auto norms = [&](int g0, int count) {
     for (int g = wave; g < count; g += 4) {
@@ -630,29 +679,6 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
     }
     __syncthreads();
   };
-  if ((int)blockIdx.z < out_groups) {
-    const int g0 = blockIdx.z * out_heads, count = min(group - g0, out_heads);
-    norms(g0, count);
-    const int cols = D / 4, each = 256 / cols / out_heads;            // rows of a head
-    const int c = tid % cols, r = tid / cols, hd = r / each, s0 = r - hd * each;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (hd < count) {
-      const float* st = wk.stat + 2 * (head0 + g0 + hd);
-      const float* part = wk.part + (head0 + g0 + hd) * D + 4 * c;
-#pragma unroll 4
-      for (int s = s0; s < parts; s += each)
-        o += *(const f32x4*)(part + (int64_t)s * a.heads * D) *
-             (st[s * stride] == -INFINITY ? 0.0f : exp2_fast(st[s * stride] - norm[hd][0]));
-    }
-    rows[tid] = o;
-    __syncthreads();
-    if (hd >= count || s0 > 0) return;
-    for (int s = 1; s < each; ++s) o += rows[tid + s * cols];
-    X* dst = (X*)((char*)a.out + (int64_t)b * a.ldo) + (int64_t)(h * group + g0 + hd) * D + 4 * c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = (X)(o[i] * norm[hd][1]);
-    return;
-  }
   for (int t0 = ((int)blockIdx.z - out_groups) * kJoinTokens; t0 < n; t0 += ((int)gridDim.z - out_groups) * kJoinTokens) {
   const int t = t0 + 4 * tid;                     // four tokens of one page
   const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);

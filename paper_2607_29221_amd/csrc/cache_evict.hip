@@ -14,6 +14,7 @@
 // the steps are launches: counts of the first, second and third digit (each
 // finds the digit before it from the counts of all chunks), then the numbering.
 #include "cache.h"
+#include "device_common.h"
 #include "dispatch.h"
 
 namespace mosaic {
@@ -88,13 +89,13 @@ __device__ __forceinline__ bool agrees(uint32_t key, uint32_t prefix, int d) {
   return d == 0 || (key >> digit_shift(d - 1)) == prefix;
 }
 
-// From counts of a digit (thread t holds those of values kBins - 1 - PER t
+// From counts of a digit (thread t holds those of values BINS - 1 - PER t
 // downwards in own[0 ..]): the value at which the running sum from the top
 // reaches `need`, and what is still needed within it. All threads.
-template <int THREADS>
-__device__ __forceinline__ void find_digit(const uint32_t (&own)[kBins / THREADS], uint32_t need, uint32_t* part,
+template <int THREADS, int BINS>
+__device__ __forceinline__ void find_digit(const uint32_t (&own)[BINS / THREADS], uint32_t need, uint32_t* part,
                                            uint32_t* found) {
-  constexpr int PER = kBins / THREADS;
+  constexpr int PER = BINS / THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t total = 0;
 #pragma unroll
@@ -113,7 +114,7 @@ __device__ __forceinline__ void find_digit(const uint32_t (&own)[kBins / THREADS
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     if (before < need && before + own[k] >= need) {
-      found[0] = (uint32_t)(kBins - 1 - PER * tid - k);
+      found[0] = (uint32_t)(BINS - 1 - PER * tid - k);
       found[1] = need - before;
     }
     before += own[k];
@@ -266,7 +267,8 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
     const int32_t evicted = n - budget;
 #pragma unroll
     for (int k = 0; k < kFew; ++k) {
-      if (k >= evicted) break;
+      out[k] = n;                                 // none
+      if (k >= evicted) continue;
       uint64_t m = ~(uint64_t)0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
     uint32_t own[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) own[k] = bins[kBins - 1 - PER * tid - k];
-    find_digit<THREADS>(own, need, part, found);
+    find_digit<THREADS, kBins>(own, need, part, found);
     prefix = prefix << (d == 2 ? 10 : 11) | found[0];
     need = found[1];
     __syncthreads();
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(kChunkThreads) void cache_count_kernel(EvictLaunch 
 #pragma unroll
       for (int k = 0; k < PER; ++k) own[k] += l.counts[D - 1][(int64_t)c * kBins + kBins - 1 - PER * tid - k];
     const uint32_t before = D > 1 ? l.found[0] : 0u;
-    find_digit<kChunkThreads>(own, D > 1 ? l.found[1] : (uint32_t)a.budget, part, found);
+    find_digit<kChunkThreads, kBins>(own, D > 1 ? l.found[1] : (uint32_t)a.budget, part, found);
     prefix = before << 11 | found[0];
     if (chunk == 0 && tid == 0) {
       l.found[2 * (D - 1)] = prefix;
@@ -402,20 +404,25 @@ __global__ __launch_bounds__(kChunkThreads) void cache_count_kernel(EvictLaunch 
   for (int k = 0; k < PER; ++k) l.counts[D][(int64_t)chunk * kBins + kChunkThreads * k + tid] = bins[kChunkThreads * k + tid];
 }
 
+// The numbering, kNumberKeys rounds of slots per workgroup (a chunk's take more
+// instructions than one compute unit should issue): rounds before its own in
+// the chunk are counted again.
+constexpr int kNumberKeys = 4, kNumberParts = kChunkKeys / kNumberKeys, kLastBins = 1024;
 __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch a, int64_t moves) {
-  constexpr int PER = kBins / kChunkThreads, NW = kChunkThreads / 64;
-  __shared__ uint32_t part[NW], found[2], cnt[NW * kChunkKeys], lower[2];
-  const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int NW = kChunkThreads / 64;
+  __shared__ uint32_t part[NW], part_equal[NW], found[2], cnt[NW * kNumberKeys], lower[2], lower_bin;
+  const int chunk = blockIdx.x / kNumberParts, round0 = blockIdx.x % kNumberParts * kNumberKeys;
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t bh = (int64_t)b * a.c.kv_heads + h;
-  const int32_t n = held_tokens(a.state, b, a.max_len), first = chunk * kChunk;
+  const int32_t n = held_tokens(a.state, b, a.max_len), chunk0 = chunk * kChunk, first = chunk0 + kChunkThreads * round0;
   int32_t* kept = a.kept != nullptr ? a.kept + bh * a.budget : nullptr;
   const bool apart = apart_of(a);
   const Lists l = lists_of(a, moves, bh);
   if (kept != nullptr)
-    for (int64_t i = n + (int64_t)chunk * kChunkThreads + tid; i < a.budget; i += (int64_t)gridDim.x * kChunkThreads) kept[i] = -1;
+    for (int64_t i = n + (int64_t)blockIdx.x * kChunkThreads + tid; i < a.budget; i += (int64_t)gridDim.x * kChunkThreads) kept[i] = -1;
   if (n <= a.budget) {
-    if (chunk == 0 && tid == 0 && moves > 0) *l.count = 0;
-    for (int32_t i = first + tid; i < min(n, first + kChunk); i += kChunkThreads) {
+    if (blockIdx.x == 0 && tid == 0 && moves > 0) *l.count = 0;
+    for (int32_t i = first + tid; i < min(n, first + kNumberKeys * kChunkThreads); i += kChunkThreads) {
       const int32_t page = page_of(a.c, b, i);
       const int64_t row = page >= 0 ? row_index(a.c, page, h, i) : -1;
       stay(a, kept, apart, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
@@ -423,57 +430,74 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
     return;
   }
   if (first >= n) return;
-  Tokens<kChunkKeys> t;
-  int32_t page[kChunkKeys];
+  uint32_t key[kChunkKeys - kNumberKeys];
+#pragma unroll
+  for (int r = 0; r < kChunkKeys - kNumberKeys; ++r) key[r] = r < round0 ? l.keys[chunk0 + kChunkThreads * r + tid] : 0u;
+  Tokens<kNumberKeys> t;
+  int32_t page[kNumberKeys];
   const bool copies = apart && first < a.budget;
 #pragma unroll
-  for (int r = 0; r < kChunkKeys; ++r) {
+  for (int r = 0; r < kNumberKeys; ++r) {
     const int32_t i = min(first + kChunkThreads * r + tid, n - 1);
     t.key[r] = l.keys[i];
     page[r] = copies ? page_of(a.c, b, i) : -1;
   }
   // the last digit, and how many of its values lie in the chunks before
   const int chunks = (n + kChunk - 1) / kChunk;
-  uint32_t own[PER] = {}, earlier[PER] = {}, above = 0;
-#pragma unroll 16
-  for (int c = 0; c < chunks; ++c)
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const uint32_t v = l.counts[2][(int64_t)c * kBins + kBins - 1 - PER * tid - k];
-      own[k] += v;
-      earlier[k] += c < chunk ? v : 0u;
-    }
+  uint32_t own[1] = {0}, earlier = 0, above = 0;
+#pragma unroll 8
+  for (int c = 0; c < chunks; ++c) {
+    const uint32_t v = l.counts[2][(int64_t)c * kBins + kLastBins - 1 - tid];
+    own[0] += v;
+    earlier += c < chunk ? v : 0u;
+  }
   for (int c = tid; c < chunk; c += kChunkThreads) above += l.above[c];
 #pragma unroll
-  for (int r = 0; r < kChunkKeys; ++r) {          // under way while the digit is found
+  for (int r = 0; r < kNumberKeys; ++r) {         // under way while the digit is found
     t.row[r] = page[r] >= 0 ? row_index(a.c, page[r], h, min(first + kChunkThreads * r + tid, n - 1)) : -1;
     t.w[r] = page[r] >= 0 ? a.c.weights[t.row[r]] : 0.0f;
     t.o[r] = page[r] >= 0 ? a.c.order[t.row[r]] : 0;
   }
-  find_digit<kChunkThreads>(own, l.found[3], part, found);
+  find_digit<kChunkThreads, kLastBins>(own, l.found[3], part, found);
   const uint32_t digit = found[0], need = found[1], least = l.found[2] << 10 | digit;
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const uint32_t value = (uint32_t)(kBins - 1 - PER * tid - k);
-    if (value > digit) above += earlier[k];
-    if (value == digit) lower[1] = earlier[k];
-  }
+  const uint32_t value = (uint32_t)(kLastBins - 1 - tid);
+  if (value > digit) above += earlier;
+  if (value == digit) lower_bin = earlier;
+  uint32_t equal = 0;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off);
+#pragma unroll
+  for (int r = 0; r < kChunkKeys - kNumberKeys; ++r)
+    if (r < round0) {
+      above += (uint32_t)__popcll(__ballot(key[r] > least));
+      equal += (uint32_t)__popcll(__ballot(key[r] == least));
+    }
   __syncthreads();
-  if (lane == 0) part[wave] = above;
+  if (lane == 0) {
+    part[wave] = above;
+    part_equal[wave] = equal;
+  }
   __syncthreads();
   if (tid == 0) {
     above = 0;
-    for (int w = 0; w < NW; ++w) above += part[w];
+    equal = lower_bin;
+    for (int w = 0; w < NW; ++w) {
+      above += part[w];
+      equal += part_equal[w];
+    }
     lower[0] = above;
+    lower[1] = equal;
   }
   __syncthreads();
-  number_slots<kChunkThreads, kChunkKeys>(a, b, h, l, kept, apart, first, n, least, need, lower[0], lower[1], t, cnt);
+  number_slots<kChunkThreads, kNumberKeys>(a, b, h, l, kept, apart, first, n, least, need, lower[0], lower[1], t, cnt);
 }
 
-// Copies rows along the pairs of slots, 16 bytes per thread.
-__global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t moves, int32_t per_block) {
+// Copies rows along the pairs of slots, 16 bytes per thread. Bound by the rows'
+// traffic: 63 MB in and out in 16 us for the 131072 -> 8192 case. Four rounds
+// per thread with all loads of a kind asked for together took 19 us: the
+// registers cost more waves than the rounds cost time.
+constexpr int32_t kMovesPerBlock = 64;
+__global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t moves) {
   const int h = blockIdx.y, b = blockIdx.z;
   const int64_t bh = (int64_t)b * a.c.kv_heads + h;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
@@ -484,8 +508,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
   }
   if (moves == 0) return;
   const Lists l = lists_of(a, moves, bh);
-  const int32_t all = *l.count, first = (int32_t)blockIdx.x * per_block;
-  const int32_t count = min(all - first, per_block);
+  const int32_t all = *l.count, first = (int32_t)blockIdx.x * kMovesPerBlock;
+  const int32_t count = min(all - first, kMovesPerBlock);
   const int32_t chunks = a.c.head_dim * (a.c.dtype == MOSAIC_F32 ? 4 : 2) / 16;
   for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {
     const int32_t m = w / chunks, c = w - m * chunks;
@@ -493,9 +517,9 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
     const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);
     if (pf < 0 || pt < 0) continue;
     const int64_t of = row_offset(a.c, pf, h, from) + 16 * c, ot = row_offset(a.c, pt, h, to) + 16 * c;
-    const uint4 k = *(const uint4*)(a.c.k + of), v = *(const uint4*)(a.c.v + of);
-    *(uint4*)(a.c.k + ot) = k;
-    *(uint4*)(a.c.v + ot) = v;
+    const u32x4 k = *(const u32x4*)(a.c.k + of), v = *(const u32x4*)(a.c.v + of);
+    *(u32x4*)(a.c.k + ot) = k;
+    *(u32x4*)(a.c.v + ot) = v;
     if (c == 0) {
       const int64_t rf = row_index(a.c, pf, h, from), rt = row_index(a.c, pt, h, to);
       a.new_weights[rt] = a.c.weights[rf];
@@ -527,13 +551,12 @@ hipError_t launch_cache_evict(const EvictLaunch& a, hipStream_t s) {
       cache_count_kernel<1><<<grid, kChunkThreads, 0, s>>>(a, moves);
       cache_count_kernel<2><<<grid, kChunkThreads, 0, s>>>(a, moves);
     }
-    cache_number_kernel<<<grid, kChunkThreads, 0, s>>>(a, moves);
+    cache_number_kernel<<<dim3(grid.x * kNumberParts, grid.y, grid.z), kChunkThreads, 0, s>>>(a, moves);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int32_t per_block = 64;
-  const unsigned blocks = moves > 0 ? (unsigned)((moves + per_block - 1) / per_block) : 1u;
-  cache_move_kernel<<<dim3(blocks, a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, moves, per_block);
+  const unsigned blocks = moves > 0 ? (unsigned)((moves + kMovesPerBlock - 1) / kMovesPerBlock) : 1u;
+  cache_move_kernel<<<dim3(blocks, a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, moves);
   return hipGetLastError();
 }
 

@@ -97,6 +97,47 @@ def test_weights_add_up(act, cache, heads, kv, dim, page):
 
 
 @pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", ((71, 1, 64), (40, 1, 128), (34, 2, 128), (20, 1, 256), (33, 1, 24)))
+def test_many_query_heads_per_key_head(act, cache, heads, kv, dim):
+    """More than 16 query heads of a group: two blocks of them in a wave, or the
+    keys and values read by several workgroups."""
+    lengths = (130, 0, 1, 700)
+    c = make_cache(lengths, kv, dim, 32, cache, 25, evicts=True)
+    before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+    q, out, scale = run(c, heads, act, 26, accumulate=True)
+    check(c, q, heads, out, act, scale, before)
+
+
+@pytest.mark.parametrize("act,cache", (("f32", "bf16"), ("f16", "f16"), ("f32", "f32")))
+@pytest.mark.parametrize("batch", (64, 65, 200))
+def test_many_sequences(act, cache, batch):
+    """More sequences than a wave has lanes, most of them short, many empty: a
+    workgroup's share holds several, and some workgroups get none."""
+    r = np.random.default_rng(batch)
+    lengths = [int(n) if r.random() < 0.6 else 0 for n in r.exponential(60, batch)]
+    lengths[0], lengths[-1], lengths[batch // 2] = 0, 0, 1500
+    c = make_cache(lengths, 2, 64, 16, cache, 27, evicts=True)
+    before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+    q, out, scale = run(c, 6, act, 28, accumulate=True)
+    check(c, q, 6, out, act, scale, before)
+
+
+@pytest.mark.parametrize("max_len", (None, 2048))
+def test_room_does_not_matter(max_len):
+    """The same tokens in tables with room for many more: the cut follows the
+    lengths, so the outputs differ by the order of sums at most."""
+    outs = []
+    c = make_cache((2000, 7, 0, 600), 2, 64, 64, "bf16", 29)
+    for room in (0, 500):
+        wide = torch.nn.functional.pad(c.block_table, (0, room), value=-1)
+        f = m.KVCache(c.k, c.v, wide, c.state)
+        q, out, scale = run(f, 8, "f32", 30, max_len=max_len)
+        check(c, q, 8, out, "f32", scale)
+        outs.append(out)
+    assert (outs[0] - outs[1]).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
 def test_long_sequences(act, cache):
     """Work split over the length: one sequence of many tokens beside short ones."""
     c = make_cache((20001, 3, 0, 4097), 2, 128, 64, cache, 31, evicts=True)
