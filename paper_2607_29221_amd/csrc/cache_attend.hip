@@ -18,10 +18,12 @@
 //   takes a value's tokens along its inner dimension: a lane loads 16 bytes
 //   of 8 tokens' rows and turns them with byte permutes (32 for 32 tokens of
 //   128), so nothing passes through LDS.
-// * Activations in float32 over a 16-bit cache keep their precision: q and p
-//   are split into 16-bit parts (three of bf16, two of f16 with the range
-//   centred) that are multiplied one after the other into the same sums. The
-//   matrix cores have room for it (a sixth of their rate at full bandwidth).
+// * Over a 16-bit cache, float32 queries and all weights are split into 16-bit
+//   parts (float32 activations: three of bf16, two of f16 with the range
+//   centred; 16-bit ones: two for the weights) that are multiplied one after
+//   the other into the same sums, so nothing but the stored types is rounded.
+//   The matrix cores have room for it (a sixth of their rate at full
+//   bandwidth): 64 sequences take 162 us with bf16 and with float32.
 // * M is raised, and O rescaled, only when a score passes it by more than
 //   kSlack: sums of up to 2^kSlack are as exact as sums of up to 1.
 // * All tokens of a key/value head, one sequence after the other, are cut into
@@ -83,7 +85,10 @@ template <int CT, int XT, int DP> struct Form {
   typedef typename FloatType<CT>::type C;
   typedef typename FloatType<XT>::type X;
   static constexpr bool kWide = CT == MOSAIC_F32;
+  // 16-bit numbers that make up a query's element (one if it is one) and a
+  // weight (16-bit activations: enough that only the output's rounding shows)
   static constexpr int kParts = kWide || XT != MOSAIC_F32 ? 1 : CT == MOSAIC_BF16 ? 3 : 2;
+  static constexpr int kWeightParts = kWide ? 1 : XT != MOSAIC_F32 || CT == MOSAIC_F16 ? 2 : 3;
   static constexpr int kSub = kWide ? 1 : 2;                // blocks of 16 tokens
   static constexpr int kTokens = 16 * kSub;
   static constexpr int kKeyLoads = DP * (int)sizeof(C) / 64;  // 16 bytes per lane and block of 16 tokens
@@ -245,7 +250,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ?
   typedef Matrix<CT> M;
   typedef typename M::Frag Frag;
   constexpr int E = F::kWide ? 4 : 8;           // elements of a 16-byte key chunk
-  constexpr int KL = F::kKeyLoads, NV = F::kValueLoads, EV = F::kEach, PARTS = F::kParts;
+  constexpr int KL = F::kKeyLoads, NV = F::kValueLoads, EV = F::kEach, PARTS = F::kParts, WPARTS = F::kWeightParts;
   constexpr int kPolicy = STREAM ? kStream : 0;
   constexpr int kHold = 8192 / 16;              // of a wave's scores, 16 bytes each
   union Shared {
@@ -480,7 +485,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ?
       holding += F::kSub;
     }
 
-    Frag pf[NT][PARTS];
+    Frag pf[NT][WPARTS];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
@@ -499,10 +504,10 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ?
       for (int i = 0; i < F::kRows; ++i) {
         const float w = exp2_fast(p[nt][i] - base[nt]);
         sum[nt] += w;
-        C part[PARTS];
-        split<C, PARTS>(w, part);
+        C part[WPARTS];
+        split<C, WPARTS>(w, part);
 #pragma unroll
-        for (int s = 0; s < PARTS; ++s) pf[nt][s][i] = part[s];
+        for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
       }
     }
 
@@ -522,7 +527,7 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ?
           vf = __builtin_bit_cast(Frag, w);
         }
 #pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part)
+        for (int part = WPARTS - 1; part >= 0; --part)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
       }
