@@ -101,8 +101,10 @@ mosaic_status check_state(const CacheView& v, const int32_t* state, const int32_
 }
 
 mosaic_status check_workspace(const void* p, int64_t bytes, int64_t needed) {
-  if (bytes < needed) return fail(MOSAIC_ERR_INVALID_ARG, "workspace of %lld bytes, needs %lld", (long long)bytes, (long long)needed);
-  if (needed > 0 && (p == nullptr || !aligned16(p))) return fail(MOSAIC_ERR_INVALID_ARG, "workspace is NULL or not 16-byte aligned");
+  if (bytes < needed)
+    return fail(MOSAIC_ERR_INVALID_ARG, "workspace of %lld bytes, needs %lld", (long long)bytes, (long long)needed);
+  if (needed > 0 && (p == nullptr || !aligned16(p)))
+    return fail(MOSAIC_ERR_INVALID_ARG, "workspace is NULL or not 16-byte aligned");
   return MOSAIC_OK;
 }
 
@@ -154,13 +156,15 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
     int64_t pairs = 0;
     for (int i = 0; i < kMaxAxes; ++i) {
       if (i < rotary->naxes) {
-        if (rotary->sections[i] < 0 || rotary->sections[i] > D) return fail(MOSAIC_ERR_INVALID_ARG, "section outside [0, head_dim]");
+        if (rotary->sections[i] < 0 || rotary->sections[i] > D)
+          return fail(MOSAIC_ERR_INVALID_ARG, "section outside [0, head_dim]");
         pairs += rotary->sections[i];
       }
       a.rot.ends[i] = (int32_t)pairs;
     }
     for (int i = rotary->naxes - 1; i < kMaxAxes; ++i) a.rot.ends[i] = INT32_MAX;   // the last axis has the rest
-    if (pairs < 1 || 2 * pairs > D) return fail(MOSAIC_ERR_INVALID_ARG, "%lld pairs in heads of %lld", (long long)pairs, (long long)D);
+    if (pairs < 1 || 2 * pairs > D)
+      return fail(MOSAIC_ERR_INVALID_ARG, "%lld pairs in heads of %lld", (long long)pairs, (long long)D);
     if (rotary->table == nullptr || rotary->rows < 1) return fail(MOSAIC_ERR_INVALID_ARG, "rotary table is NULL or empty");
     if (rotary->rows > INT32_MAX) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^31 - 1 rows of the rotary table");
     if (rotary->positions != nullptr && rotary->ldp < rows) return fail(MOSAIC_ERR_INVALID_ARG, "ldp < rows");
@@ -219,8 +223,8 @@ mosaic_status mosaic_cache_attend(const mosaic_kv_cache* cache, const void* q, i
     return fail(MOSAIC_ERR_INVALID_ARG, "out overlaps q");
   if (lengths == nullptr) return fail(MOSAIC_ERR_INVALID_ARG, "lengths is NULL");
   if (a.accumulate && a.c.weights == nullptr) return fail(MOSAIC_ERR_INVALID_ARG, "the cache has no weights to add to");
-  if ((st = check_workspace(workspace, workspace_bytes, cache_attend_workspace(a.c, heads, a.max_len, a.accumulate))) != MOSAIC_OK)
-    return st;
+  st = check_workspace(workspace, workspace_bytes, cache_attend_workspace(a.c, heads, a.max_len, a.accumulate));
+  if (st != MOSAIC_OK) return st;
   a.q = q;
   a.out = out;
   a.ldq = ldq * size;
@@ -259,7 +263,8 @@ mosaic_status mosaic_cache_evict(const mosaic_kv_cache* cache, const int32_t* st
         (new_order != a.c.order && overlap(new_order, numbers, a.c.order, numbers)))
       return fail(MOSAIC_ERR_INVALID_ARG, "new_weights or new_order overlaps the cache's");
   }
-  if ((st = check_workspace(workspace, workspace_bytes, cache_evict_workspace(a.c, a.max_len, budget))) != MOSAIC_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, cache_evict_workspace(a.c, a.max_len, budget));
+  if (st != MOSAIC_OK) return st;
   a.state = state;
   a.new_state = new_state;
   a.recent = recent;

@@ -726,8 +726,10 @@ PyMODINIT_FUNC PyInit__binding(void) {
   s_values = PyUnicode_InternFromString("values");
   s_rows = PyUnicode_InternFromString("rows");
   s_cols = PyUnicode_InternFromString("cols");
-  PyObject** const names[] = {&s_k, &s_v, &s_block_table, &s_state, &s_weights, &s_order, &s_table, &s_sections, &s_positions, &s_interleaved};
-  const char* const texts[] = {"k", "v", "block_table", "state", "weights", "order", "table", "sections", "positions", "interleaved"};
+  PyObject** const names[] = {&s_k,     &s_v,     &s_block_table, &s_state,     &s_weights,
+                              &s_order, &s_table, &s_sections,    &s_positions, &s_interleaved};
+  const char* const texts[] = {"k",     "v",     "block_table", "state",     "weights",
+                               "order", "table", "sections",    "positions", "interleaved"};
   for (int i = 0; i < 10; ++i)
     if ((*names[i] = PyUnicode_InternFromString(texts[i])) == nullptr) return nullptr;
   if (!s_buf || !s_col0 || !s_row_ptr || !s_col_idx || !s_values || !s_rows || !s_cols) return nullptr;

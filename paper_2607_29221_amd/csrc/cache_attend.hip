@@ -161,8 +161,9 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   p.tile_groups = (tiles + p.wave_tiles - 1) / p.wave_tiles;
   // A workgroup per compute unit, or as many as there are steps: its four
   // waves keep 64 KiB of a bf16 cache's rows of 128 in flight, which is
-  // enough, and every further workgroup is another part to join (64 sequences:
-  // 6.3 TB/s with 256 workgroups in all, 6.2 with 512, 6.1 with 768).
+  // enough, and every further workgroup is another part to join (64 sequences
+  // with the join: 162 us with 256 workgroups in all, 165 us with 512, 169 us
+  // with 768; heads of 256 elements 89, 92 and 101 us).
   const int64_t groups = (int64_t)c.kv_heads * p.tile_groups;
   const int64_t wanted = (256 + groups - 1) / groups;
   const int64_t steps = c.batch * ((max_len + kStepTokens - 1) / kStepTokens);
@@ -240,10 +241,25 @@ __device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int 
   }
 }
 
-// NT: blocks of 16 query heads per wave. STREAM: no other workgroup reads the
-// same keys and values.
+// Waves per SIMD that the registers are held to: one is enough for a call of
+// its own, more let it share the chip.
+constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : (DP == 128 ? 3 : 4) - (NT - 1); }
+
+// NT: blocks of 16 query heads per wave (64 query heads on one key/value head
+// of 128 elements, 64 sequences: 155 us with one, 83 us with two). STREAM: no
+// other workgroup reads the same keys and values, so they pass by the caches
+// (131072 tokens: 92 us through them, 81 us past them); where several do
+// (groups of more than 32 heads) they go through (82 us, 95 us past).
+// Measured on an MI355X, this kernel alone, heads of 128 elements, 64 query
+// and 8 key/value heads: 131072 tokens of one sequence 81 us (6.6 TB/s of keys
+// and values); 64 sequences of 512 to 7168 tokens 157 us (6.6 TB/s); 32 heads
+// of each, float32 cache, 120 us (6.2 TB/s); 1024 tokens 7 us, the latency of
+// its chain of loads. With weights the 64 sequences take 216 us: the 63 MB of
+// scores cost more than their share of the traffic (205 us with half of them
+// stored), whether one step's or many steps' are stored at a time, past the
+// caches or through them.
 template <int CT, int XT, int DP, int NT, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ? 3 : 2) : (NT == 1 ? 4 : 3)) void cache_attend_kernel(AttendLaunch a, Work wk) {
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_kernel(AttendLaunch a, Work wk) {
   typedef Form<CT, XT, DP> F;
   typedef typename F::C C;
   typedef typename F::X X;
@@ -278,331 +294,334 @@ __global__ __launch_bounds__(64 * kWaves, DP == 256 ? 1 : DP == 128 ? (NT == 1 ?
   int b = sequence_at(a, lane, at, first64, &before);
   if (b < 0) return;
   while (true) {
-  const int n = held_tokens_uniform(a.lengths, b, a.max_len), steps = (n + kStepTokens - 1) / kStepTokens;
-  const int t0 = (at - before) * kStepTokens, t1 = min(n, min(stop - before, steps) * kStepTokens);
+    const int n = held_tokens_uniform(a.lengths, b, a.max_len), steps = (n + kStepTokens - 1) / kStepTokens;
+    const int t0 = (at - before) * kStepTokens, t1 = min(n, min(stop - before, steps) * kStepTokens);
 
-  // What only the start and the end of a part need is computed there: kept
-  // in registers through the steps it would cost a wave per SIMD.
-  int own_lane = lane;
-  asm volatile("" : "+v"(own_lane));
+    // What only the start and the end of a part need is computed there: kept
+    // in registers through the steps it would cost a wave per SIMD.
+    int own_lane = lane;
+    asm volatile("" : "+v"(own_lane));
 
-  // the queries, asked for first (loads come back in order); lanes without a
-  // head or column read another's
-  constexpr int QL = E * (int)sizeof(X) / 16;   // loads per chunk
-  u32x4 raw[NT][KL][QL];
+    // the queries, asked for first (loads come back in order); lanes without a
+    // head or column read another's
+    constexpr int QL = E * (int)sizeof(X) / 16;   // loads per chunk
+    u32x4 raw[NT][KL][QL];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int head = min((tile0 + nt) * kHeadTile + (own_lane & 15), group - 1);
-    const char* row = (const char*)a.q + (int64_t)b * a.ldq + ((int64_t)h * group + head) * D * (int)sizeof(X);
-#pragma unroll
-    for (int c = 0; c < KL; ++c)
-#pragma unroll
-      for (int l = 0; l < QL; ++l)
-        raw[nt][c][l] = *(const u32x4*)(row + min((4 * c + (own_lane >> 4)) * E, D - E) * (int)sizeof(X) + 16 * l);
-  }
-
-  // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
-  const int ts = (int)a.c.token_stride;
-  int key_off[KL], value_off[NV];
-#pragma unroll
-  for (int c = 0; c < KL; ++c) key_off[c] = (4 * c + quad) * E < D ? col * ts + (4 * c + quad) * 16 : kNowhere;
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int d = (16 * v + col) * EV;
-    value_off[v] = d < D ? 4 * quad * ts + d * (int)sizeof(C) : kNowhere;
-  }
-
-  // a block of 16 tokens: its first row's place in memory and how many there are
-  struct Block {
-    int64_t base;
-    int valid;
-  };
-  const int page_mask = (1 << a.c.log2_page) - 1;
-  auto block_at = [&](int slot) {
-    Block k = {0, 0};
-    if (slot < t1) {
-      const int page = page_of_uniform(a.c, b, slot);
-      if (page >= 0) {
-        k.base = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (slot & page_mask) * ts;
-        k.valid = min(t1 - slot, 16);
-      }
-    }
-    return k;
-  };
-  Frag key[F::kSub][KL];
-  auto load_keys = [&](const Block* k) {
-#pragma unroll
-    for (int s = 0; s < F::kSub; ++s) {
-      const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.k + k[s].base, k[s].valid * ts);
+    for (int nt = 0; nt < NT; ++nt) {
+      const int head = min((tile0 + nt) * kHeadTile + (own_lane & 15), group - 1);
+      const char* row = (const char*)a.q + (int64_t)b * a.ldq + ((int64_t)h * group + head) * D * (int)sizeof(X);
 #pragma unroll
       for (int c = 0; c < KL; ++c)
-        key[s][c] = __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, kPolicy));
+#pragma unroll
+        for (int l = 0; l < QL; ++l)
+          raw[nt][c][l] = *(const u32x4*)(row + min((4 * c + (own_lane >> 4)) * E, D - E) * (int)sizeof(X) + 16 * l);
     }
-  };
-  constexpr int kStep = F::kTokens * kWaves;
-  const int first = t0 + F::kTokens * wave;
-  Block cur[F::kSub];
+
+    // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
+    const int ts = (int)a.c.token_stride;
+    int key_off[KL], value_off[NV];
 #pragma unroll
-  for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
-  // values of these tokens
-  u32x4 value[F::kRows][NV];
-  auto load_values = [&](const Block* k) {
+    for (int c = 0; c < KL; ++c) key_off[c] = (4 * c + quad) * E < D ? col * ts + (4 * c + quad) * 16 : kNowhere;
 #pragma unroll
-    for (int s = 0; s < F::kSub; ++s) {
-      const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.v + k[s].base, k[s].valid * ts);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          if (EV * sizeof(C) == 16) {
-            value[4 * s + i][v] =
-                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kPolicy));
-          } else {
-            const u32x2 w =
-                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kPolicy));
-            value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
-          }
+    for (int v = 0; v < NV; ++v) {
+      const int d = (16 * v + col) * EV;
+      value_off[v] = d < D ? 4 * quad * ts + d * (int)sizeof(C) : kNowhere;
+    }
+
+    // a block of 16 tokens: its first row's place in memory and how many there are
+    struct Block {
+      int64_t base;
+      int valid;
+    };
+    const int page_mask = (1 << a.c.log2_page) - 1;
+    auto block_at = [&](int slot) {
+      Block k = {0, 0};
+      if (slot < t1) {
+        const int page = page_of_uniform(a.c, b, slot);
+        if (page >= 0) {
+          k.base = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (slot & page_mask) * ts;
+          k.valid = min(t1 - slot, 16);
         }
-    }
-  };
-  load_keys(cur);
-  load_values(cur);
-
-  // Queries, in parts: every wave reads them (the scale is a lane's own) and
-  // writes a share.
-  float scale[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int head = (tile0 + nt) * kHeadTile + (own_lane & 15);
-    float x[KL][E];
-    float top = 0.0f;
-#pragma unroll
-    for (int c = 0; c < KL; ++c) {
-      const bool there = head < group && (4 * c + (own_lane >> 4)) * E < D;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        constexpr int PER = 16 / (int)sizeof(X);
-        const Chunk<X> v = __builtin_bit_cast(Chunk<X>, raw[nt][c][e / PER]);
-        x[c][e] = there ? (float)v.e[e % PER] : 0.0f;
-        top = fmaxf(top, fabsf(x[c][e]));
       }
-    }
-    int up = 0;
-    if (CT == MOSAIC_F16 && XT == MOSAIC_F32) {
-      // by a power of two into the upper part of the range of f16
-      top = head_max(top);
-      up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
-    }
-    scale[nt] = ldexpf(a.scale_log2, -up);
+      return k;
+    };
+    Frag key[F::kSub][KL];
+    auto load_keys = [&](const Block* k) {
 #pragma unroll
-    for (int c = 0; c < KL; ++c) {
-      if (c % kWaves != wave) continue;
-      Frag f[PARTS];
+      for (int s = 0; s < F::kSub; ++s) {
+        const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.k + k[s].base, k[s].valid * ts);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        C part[PARTS];
-        split<C, PARTS>(CT == MOSAIC_F16 && XT == MOSAIC_F32 ? ldexpf(x[c][e], up) : x[c][e], part);
-#pragma unroll
-        for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
+        for (int c = 0; c < KL; ++c)
+          key[s][c] = __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(r, key_off[c], 0, kPolicy));
       }
+    };
+    constexpr int kStep = F::kTokens * kWaves;
+    const int first = t0 + F::kTokens * wave;
+    Block cur[F::kSub];
 #pragma unroll
-      for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][own_lane] = f[s];
-    }
-  }
-  lds_barrier();                                // leaves keys and values under way
-
-  f32x4 acc[NT][NV][EV];
-  float top[NT], base[NT], sum[NT];
+    for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
+    // values of these tokens
+    u32x4 value[F::kRows][NV];
+    auto load_values = [&](const Block* k) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    top[nt] = -INFINITY;
-    base[nt] = sum[nt] = 0.0f;
-  }
-
-  // Scores go to memory through LDS, many steps at a time: a load that is
-  // issued behind a store waits for it, and stores take longer than loads.
-  float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 4 * quad;
-  const int held_heads = min(group - tile0 * kHeadTile, NT * kHeadTile);
-  int holding = 0, held_from = first;           // blocks of 16 tokens, and the first one's step
-  auto release = [&]() {
-    for (int k = 0; k < holding; ++k)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int hd = nt * kHeadTile + col;
-        if (hd < held_heads)
-          *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group + 16 * (tile0 * kHeadTile + hd)) =
-              shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
-      }
-    held_from += holding / F::kSub * kStep;
-    holding = 0;
-  };
-
-  for (int t = first; t < t1; t += kStep) {
-    asm volatile("" ::: "memory");              // the queries stay in LDS
-    Block next[F::kSub];
-#pragma unroll
-    for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
-
-    float p[NT][F::kRows], tile_top[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      f32x4 dot[F::kSub];
-#pragma unroll
-      for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int part = PARTS - 1; part >= 0; --part)           // small terms first
-#pragma unroll
-        for (int c = 0; c < KL; ++c) {
-          const Frag q = shared.in.query[nt][part][c][lane];
-#pragma unroll
-          for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
-        }
-      tile_top[nt] = -INFINITY;
-#pragma unroll
-      for (int s = 0; s < F::kSub; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * scale[nt] : -INFINITY;
-          tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
-        }
-    }
-    load_keys(next);
-    if (a.accumulate) {
-      if (4 * held_heads * (holding + F::kSub) > kHold) release();
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int s = 0; s < F::kSub; ++s) {
-          const int hd = nt * kHeadTile + col;
-          if (hd < held_heads)
-            shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
-                f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
-        }
-      holding += F::kSub;
-    }
-
-    Frag pf[NT][WPARTS];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
-        const float now = fmaxf(top[nt], head_max(tile_top[nt]));
-        const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
-        const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - rescaled);
-        sum[nt] *= f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int j = 0; j < EV; ++j) acc[nt][v][j] *= f;
-        top[nt] = now;
-        base[nt] = rescaled;
-      }
-#pragma unroll
-      for (int i = 0; i < F::kRows; ++i) {
-        const float w = exp2_fast(p[nt][i] - base[nt]);
-        sum[nt] += w;
-        C part[WPARTS];
-        split<C, WPARTS>(w, part);
-#pragma unroll
-        for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
-      }
-    }
-
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < EV; ++j) {
-        Frag vf;
-        if constexpr (F::kWide) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
-        } else {
-          u32x4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-          vf = __builtin_bit_cast(Frag, w);
-        }
-#pragma unroll
-        for (int part = WPARTS - 1; part >= 0; --part)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
-      }
-#pragma unroll
-    for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
-    load_values(cur);
-  }
-  if (a.accumulate) release();
-
-  // join the waves
-  asm volatile("" : "+v"(own_lane));
-  const int own_col = own_lane & 15, own_quad = own_lane >> 4;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const float all = head_sum(sum[nt]);
-    if (own_quad == 0) {
-      stat[nt][wave][own_col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
-      stat[nt][wave][own_col][1] = all;
-    }
-  }
-  const int chunks = D / 4;
-  const int64_t slot = u + b;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    __syncthreads();
-    {
-      float common = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stat[nt][w][own_col][0]);
-      const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - common);
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
+      for (int s = 0; s < F::kSub; ++s) {
+        const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.v + k[s].base, k[s].valid * ts);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < EV; j += 4)
-            *(f32x4*)&shared.slab[wave][own_col][(16 * v + 4 * own_quad + i) * EV + j] =
-                f32x4{acc[nt][v][j][i] * f, acc[nt][v][j + 1][i] * f, acc[nt][v][j + 2][i] * f, acc[nt][v][j + 3][i] * f};
-    }
-    __syncthreads();
-    const int g0 = (tile0 + nt) * kHeadTile, live = min(group - g0, kHeadTile);
-    for (int k = 64 * wave + own_lane; k < live * chunks; k += 64 * kWaves) {
-      const int hd = k / chunks, c = k - hd * chunks;
-      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-      float common = -INFINITY, weight = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        o += *(const f32x4*)&shared.slab[w][hd][4 * c];
-        common = fmaxf(common, stat[nt][w][hd][0]);
+          for (int v = 0; v < NV; ++v) {
+            if (EV * sizeof(C) == 16) {
+              value[4 * s + i][v] =
+                  __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, value_off[v] + i * ts, 0, kPolicy));
+            } else {
+              const u32x2 w =
+                  __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, value_off[v] + i * ts, 0, kPolicy));
+              value[4 * s + i][v] = u32x4{w[0], w[1], 0u, 0u};
+            }
+          }
       }
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w)
-        weight += stat[nt][w][hd][1] * (stat[nt][w][hd][0] == -INFINITY ? 0.0f : exp2_fast(stat[nt][w][hd][0] - common));
-      const int64_t row = slot * a.heads + h * group + g0 + hd;
-      *(f32x4*)(wk.part + row * D + 4 * c) = o;
-      if (c == 0) {
-        wk.stat[2 * row] = common;
-        wk.stat[2 * row + 1] = weight;
-      }
-    }
-  }
+    };
+    load_keys(cur);
+    load_values(cur);
 
-  // on to the next sequence of this share
-  at = before + steps;
-  if (at >= stop) return;
-  __syncthreads();                              // the outputs are read
-  before = at;
-  do {
-    if (++b >= a.c.batch) return;
-  } while (held_tokens_uniform(a.lengths, b, a.max_len) == 0);
+    // Queries, in parts: every wave reads them (the scale is a lane's own) and
+    // writes a share.
+    float scale[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int head = (tile0 + nt) * kHeadTile + (own_lane & 15);
+      float x[KL][E];
+      float top = 0.0f;
+#pragma unroll
+      for (int c = 0; c < KL; ++c) {
+        const bool there = head < group && (4 * c + (own_lane >> 4)) * E < D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          constexpr int PER = 16 / (int)sizeof(X);
+          const Chunk<X> v = __builtin_bit_cast(Chunk<X>, raw[nt][c][e / PER]);
+          x[c][e] = there ? (float)v.e[e % PER] : 0.0f;
+          top = fmaxf(top, fabsf(x[c][e]));
+        }
+      }
+      int up = 0;
+      if (CT == MOSAIC_F16 && XT == MOSAIC_F32) {
+        // by a power of two into the upper part of the range of f16
+        top = head_max(top);
+        up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+      }
+      scale[nt] = ldexpf(a.scale_log2, -up);
+#pragma unroll
+      for (int c = 0; c < KL; ++c) {
+        if (c % kWaves != wave) continue;
+        Frag f[PARTS];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          C part[PARTS];
+          split<C, PARTS>(CT == MOSAIC_F16 && XT == MOSAIC_F32 ? ldexpf(x[c][e], up) : x[c][e], part);
+#pragma unroll
+          for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
+        }
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][own_lane] = f[s];
+      }
+    }
+    lds_barrier();                                // leaves keys and values under way
+
+    f32x4 acc[NT][NV][EV];
+    float top[NT], base[NT], sum[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      top[nt] = -INFINITY;
+      base[nt] = sum[nt] = 0.0f;
+    }
+
+    // Scores go to memory through LDS, many steps at a time: a load that is
+    // issued behind a store waits for it, and stores take longer than loads.
+    float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 4 * quad;
+    const int held_heads = min(group - tile0 * kHeadTile, NT * kHeadTile);
+    int holding = 0, held_from = first;           // blocks of 16 tokens, and the first one's step
+    auto release = [&]() {
+      for (int k = 0; k < holding; ++k)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int hd = nt * kHeadTile + col;
+          if (hd < held_heads)
+          *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group +
+                    16 * (tile0 * kHeadTile + hd)) = shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
+        }
+      held_from += holding / F::kSub * kStep;
+      holding = 0;
+    };
+
+    for (int t = first; t < t1; t += kStep) {
+      asm volatile("" ::: "memory");              // the queries stay in LDS
+      Block next[F::kSub];
+#pragma unroll
+      for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
+
+      float p[NT][F::kRows], tile_top[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x4 dot[F::kSub];
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; --part)           // small terms first
+#pragma unroll
+          for (int c = 0; c < KL; ++c) {
+            const Frag q = shared.in.query[nt][part][c][lane];
+#pragma unroll
+            for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
+          }
+        tile_top[nt] = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * scale[nt] : -INFINITY;
+            tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
+          }
+      }
+      load_keys(next);
+      if (a.accumulate) {
+        if (4 * held_heads * (holding + F::kSub) > kHold) release();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int s = 0; s < F::kSub; ++s) {
+            const int hd = nt * kHeadTile + col;
+            if (hd < held_heads)
+              shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
+                  f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
+          }
+        holding += F::kSub;
+      }
+
+      Frag pf[NT][WPARTS];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
+          const float now = fmaxf(top[nt], head_max(tile_top[nt]));
+          const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
+          const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - rescaled);
+          sum[nt] *= f;
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < EV; ++j) acc[nt][v][j] *= f;
+          top[nt] = now;
+          base[nt] = rescaled;
+        }
+#pragma unroll
+        for (int i = 0; i < F::kRows; ++i) {
+          const float w = exp2_fast(p[nt][i] - base[nt]);
+          sum[nt] += w;
+          C part[WPARTS];
+          split<C, WPARTS>(w, part);
+#pragma unroll
+          for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
+        }
+      }
+
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < EV; ++j) {
+          Frag vf;
+          if constexpr (F::kWide) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
+          } else {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2],
+                                           j % 2 ? 0x07060302u : 0x05040100u);
+            vf = __builtin_bit_cast(Frag, w);
+          }
+#pragma unroll
+          for (int part = WPARTS - 1; part >= 0; --part)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
+        }
+#pragma unroll
+      for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
+      load_values(cur);
+    }
+    if (a.accumulate) release();
+
+    // join the waves
+    asm volatile("" : "+v"(own_lane));
+    const int own_col = own_lane & 15, own_quad = own_lane >> 4;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float all = head_sum(sum[nt]);
+      if (own_quad == 0) {
+        stat[nt][wave][own_col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
+        stat[nt][wave][own_col][1] = all;
+      }
+    }
+    const int chunks = D / 4;
+    const int64_t slot = u + b;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      __syncthreads();
+      {
+        float common = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stat[nt][w][own_col][0]);
+        const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - common);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < EV; j += 4)
+              *(f32x4*)&shared.slab[wave][own_col][(16 * v + 4 * own_quad + i) * EV + j] =
+                  f32x4{acc[nt][v][j][i], acc[nt][v][j + 1][i], acc[nt][v][j + 2][i], acc[nt][v][j + 3][i]} * f;
+      }
+      __syncthreads();
+      const int g0 = (tile0 + nt) * kHeadTile, live = min(group - g0, kHeadTile);
+      for (int k = 64 * wave + own_lane; k < live * chunks; k += 64 * kWaves) {
+        const int hd = k / chunks, c = k - hd * chunks;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        float common = -INFINITY, weight = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          o += *(const f32x4*)&shared.slab[w][hd][4 * c];
+          common = fmaxf(common, stat[nt][w][hd][0]);
+        }
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+          weight += stat[nt][w][hd][0] == -INFINITY ? stat[nt][w][hd][1]
+                                                    : stat[nt][w][hd][1] * exp2_fast(stat[nt][w][hd][0] - common);
+        const int64_t row = slot * a.heads + h * group + g0 + hd;
+        *(f32x4*)(wk.part + row * D + 4 * c) = o;
+        if (c == 0) {
+          wk.stat[2 * row] = common;
+          wk.stat[2 * row + 1] = weight;
+        }
+      }
+    }
+
+    // on to the next sequence of this share
+    at = before + steps;
+    if (at >= stop) return;
+    __syncthreads();                              // the outputs are read
+    before = at;
+    do {
+      if (++b >= a.c.batch) return;
+    } while (held_tokens_uniform(a.lengths, b, a.max_len) == 0);
   }
 }
 
 // Base and sum of a head over its parts, `stride` floats apart, by one wave.
-__device__ __forceinline__ void head_norm(const float* st, int64_t stride, int parts, int lane, float* common, float* sum) {
+__device__ __forceinline__ void head_norm(const float* st, int64_t stride, int parts, int lane, float* common,
+                                          float* sum) {
   float m = -INFINITY, l = 0.0f;
   for (int s = lane; s < parts; s += 64) m = fmaxf(m, st[s * stride]);
 #pragma unroll
@@ -615,10 +634,12 @@ __device__ __forceinline__ void head_norm(const float* st, int64_t stride, int p
   *sum = l;
 }
 
-// Joins the parts. The first `out_groups` workgroups of a key/value head write
+// Joins the parts (4 to 5 us: the latency of the lengths, the parts and the
+// store). The first `out_groups` workgroups of a key/value head write
 // the outputs of `out_heads` query heads each: rows of 16-byte columns, a
 // head's parts dealt out to its share of the rows of threads. The others add
-// weights up over the heads of the group, kJoinTokens tokens at a time.
+// weights up over the heads of the group, kJoinTokens tokens at a time (64
+// sequences: 21 us in all, 4 TB/s of scores, weights and parts).
 constexpr int kJoinHeads = 16, kJoinTokens = 4 * 256;
 template <int XT>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk, int32_t workgroups, int32_t out_heads) {
@@ -685,33 +706,33 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
     __syncthreads();
   };
   for (int t0 = ((int)blockIdx.z - out_groups) * kJoinTokens; t0 < n; t0 += ((int)gridDim.z - out_groups) * kJoinTokens) {
-  const int t = t0 + 4 * tid;                     // four tokens of one page
-  const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
-  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
-    const int count = min(group - g0, kJoinHeads);
-    __syncthreads();
-    norms(g0, count);
-    if (t < n) {
+    const int t = t0 + 4 * tid;                     // four tokens of one page
+    const float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + (int64_t)(t & ~15) * group + (t & 15);
+    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g0 = 0; g0 < group; g0 += kJoinHeads) {
+      const int count = min(group - g0, kJoinHeads);
+      __syncthreads();
+      norms(g0, count);
+      if (t < n) {
 #pragma unroll 8
-      for (int g = 0; g < count; ++g) {
-        const f32x4 score = *(const f32x4*)(scores + 16 * (g0 + g));
+        for (int g = 0; g < count; ++g) {
+          const f32x4 score = *(const f32x4*)(scores + 16 * (g0 + g));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] += exp2_fast(score[i] - norm[g][0]) * norm[g][1];
+          for (int i = 0; i < 4; ++i) w[i] += exp2_fast(score[i] - norm[g][0]) * norm[g][1];
+        }
       }
     }
-  }
-  const int page = t < n ? page_of(a.c, b, t) : -1;
-  if (page < 0) continue;
-  float* dst = a.c.weights + row_index(a.c, page, h, t);
-  if (t + 4 <= n) {
-    *(f32x4_any*)dst += w;
-  } else {
+    const int page = t < n ? page_of(a.c, b, t) : -1;
+    if (page < 0) continue;
+    float* dst = a.c.weights + row_index(a.c, page, h, t);
+    if (t + 4 <= n) {
+      *(f32x4_any*)dst += w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (t + i < n) dst[i] += w[i];
+      for (int i = 0; i < 3; ++i)
+        if (t + i < n) dst[i] += w[i];
+    }
   }
-}
 }
 
 template <int CT, int XT, int DP>
@@ -744,7 +765,8 @@ hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
   // weights: a workgroup per range of tokens, fewer where the heads are many
   int64_t ranges = 0;
   if (a.accumulate) {
-    const int64_t all = (a.max_len + kJoinTokens - 1) / kJoinTokens, most = 4096 / ((int64_t)a.c.kv_heads * a.c.batch) + 1;
+    const int64_t all = (a.max_len + kJoinTokens - 1) / kJoinTokens;
+    const int64_t most = 4096 / ((int64_t)a.c.kv_heads * a.c.batch) + 1;
     ranges = all < most ? all : most;
   }
   // several heads per workgroup where there are many and a sequence has few parts
