@@ -124,6 +124,21 @@ __device__ __forceinline__ int64_t row_index(const CacheView& c, int32_t page, i
   return (((int64_t)page * c.kv_heads + head) << c.log2_page) + (slot & ((1 << c.log2_page) - 1));
 }
 
+// Sums of v over the lanes up to this one: within rows of 16 by shifts, then
+// across rows.
+template <int CTRL, int ROWS> __device__ __forceinline__ int lanes_before(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v += lanes_before<0x111, 0xF>(v);
+  v += lanes_before<0x112, 0xF>(v);
+  v += lanes_before<0x114, 0xF>(v);
+  v += lanes_before<0x118, 0xF>(v);
+  v += lanes_before<0x142, 0xA>(v);       // a row's last lane to the next row (rows 1 and 3)
+  v += lanes_before<0x143, 0xC>(v);       // lane 31 to rows 2 and 3
+  return v;
+}
+
 #endif
 
 }  // namespace mosaic

@@ -185,21 +185,6 @@ int64_t part_floats(const CacheView& c, int32_t heads, const Plan& p) {
 __device__ __forceinline__ int steps_of(const AttendLaunch& a, int i) {
   return i < a.c.batch ? (held_tokens(a.lengths, i, a.max_len) + kStepTokens - 1) / kStepTokens : 0;
 }
-// Sums of v over the lanes up to this one: within rows of 16 by shifts, then
-// across rows.
-template <int CTRL, int ROWS> __device__ __forceinline__ int lanes_before(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
-}
-__device__ __forceinline__ int wave_scan(int v) {
-  v += lanes_before<0x111, 0xF>(v);
-  v += lanes_before<0x112, 0xF>(v);
-  v += lanes_before<0x114, 0xF>(v);
-  v += lanes_before<0x118, 0xF>(v);
-  v += lanes_before<0x142, 0xA>(v);       // a row's last lane to the next row (rows 1 and 3)
-  v += lanes_before<0x143, 0xC>(v);       // lane 31 to rows 2 and 3
-  return v;
-}
-
 // Steps of the first 64 sequences, a lane each: its own, and all up to it.
 struct FirstSteps {
   int own, upto;

@@ -15,12 +15,12 @@
 // finds the digit before it from the counts of all chunks), then the numbering.
 //
 // Measured on an MI355X, 8 key/value heads: 64 sequences of 2049 tokens to
-// 2048: 8.6 us for the selection (21 MB of weights, order and slots in and
+// 2048: 8.7 us for the selection (21 MB of weights, order and slots in and
 // out: 2.4 TB/s, half of it latency) and 3 us for one row per head; four of up
-// to 7168 to 1024: 12 us, the latency of its steps on 32 workgroups, and 14.5
-// us for 59 MB of float32 rows; one of 131072 to 8192: 7 + 6 + 6.5 + 10 us in
-// place of 353 us for one workgroup per head with its keys in memory, and 16
-// us for 63 MB of rows.
+// to 7168 to 1024: 11.4 us, the latency of its steps on 32 workgroups, and
+// 11.7 us for 50 MB of float32 rows; one of 131072 to 8192: 7 + 6.4 + 6.8 + 9
+// us in place of 353 us for one workgroup per head with its keys in memory,
+// and 15 us for 62 MB of rows.
 #include "cache.h"
 #include "device_common.h"
 #include "dispatch.h"
@@ -110,12 +110,7 @@ __device__ __forceinline__ void find_digit(const uint32_t (&own)[BINS / THREADS]
   uint32_t total = 0;
 #pragma unroll
   for (int k = 0; k < PER; ++k) total += own[k];
-  uint32_t sum = total;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t o = __shfl_up(sum, off);
-    if (lane >= off) sum += o;
-  }
+  const uint32_t sum = (uint32_t)wave_scan((int)total);
   if (lane == 63) part[wave] = sum;
   __syncthreads();
   uint32_t before = sum - total;
@@ -198,13 +193,7 @@ __device__ __forceinline__ void number_slots(const EvictLaunch& a, int b, int h,
       v[k] = at < ENTRIES ? cnt[at] : 0u;
       sum += v[k];
     }
-    uint32_t run = sum;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const uint32_t o = __shfl_up(run, off);
-      if (lane >= off) run += o;
-    }
-    run -= sum;
+    uint32_t run = (uint32_t)wave_scan((int)sum) - sum;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       if (EACH * lane + k < ENTRIES) cnt[EACH * lane + k] = run;
@@ -247,8 +236,8 @@ __device__ __forceinline__ bool apart_of(const EvictLaunch& a) {
 template <int THREADS, int R>
 __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, int64_t moves) {
   constexpr int NW = THREADS / 64, PER = kBins / THREADS;
-  __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t part[NW], found[2], cnt[NW * R];
+  __shared__ uint32_t bins[3][kBins];             // a digit's each, so that none waits to be cleared
+  __shared__ uint32_t part[3][NW], found[3][2], cnt[NW * R];
   __shared__ uint64_t worst[NW];
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t bh = (int64_t)b * a.c.kv_heads + h;
@@ -329,21 +318,22 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
 
   uint32_t prefix = 0, need = (uint32_t)budget;
 #pragma unroll
+  for (int d = 0; d < 3; ++d)
+#pragma unroll
+    for (int k = 0; k < PER; ++k) bins[d][THREADS * k + tid] = 0u;
+  __syncthreads();
+#pragma unroll
   for (int d = 0; d < 3; ++d) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) bins[THREADS * k + tid] = 0u;
-    __syncthreads();
-#pragma unroll
     for (int r = 0; r < R; ++r)
-      if (THREADS * r + tid < n && agrees(t.key[r], prefix, d)) atomicAdd(&bins[digit_of(t.key[r], d)], 1u);
+      if (THREADS * r + tid < n && agrees(t.key[r], prefix, d)) atomicAdd(&bins[d][digit_of(t.key[r], d)], 1u);
     __syncthreads();
     uint32_t own[PER];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) own[k] = bins[kBins - 1 - PER * tid - k];
-    find_digit<THREADS, kBins>(own, need, part, found);
-    prefix = prefix << (d == 2 ? 10 : 11) | found[0];
-    need = found[1];
-    __syncthreads();
+    for (int k = 0; k < PER; ++k) own[k] = bins[d][kBins - 1 - PER * tid - k];
+    find_digit<THREADS, kBins>(own, need, part[d], found[d]);
+    prefix = prefix << (d == 2 ? 10 : 11) | found[d][0];
+    need = found[d][1];
   }
   number_slots<THREADS, R>(a, b, h, l, kept, apart, 0, n, prefix, need, 0u, 0u, t, cnt);
 }
@@ -506,10 +496,9 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
 }
 
 // Copies rows along the pairs of slots, 16 bytes per thread. Bound by the rows'
-// traffic: 63 MB in and out in 16 us for the 131072 -> 8192 case. Four rounds
-// per thread with all loads of a kind asked for together took 19 us: the
-// registers cost more waves than the rounds cost time.
-constexpr int32_t kMovesPerBlock = 64;
+// traffic: 63 MB in and out in 14.7 us for the 131072 -> 8192 case, in 16.4 us
+// with 64 moves per workgroup (more rounds of dependent loads for a thread).
+constexpr int32_t kMovesPerBlock = 16;
 __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t moves) {
   const int h = blockIdx.y, b = blockIdx.z;
   const int64_t bh = (int64_t)b * a.c.kv_heads + h;
