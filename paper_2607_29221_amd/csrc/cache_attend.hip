@@ -435,8 +435,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
         for (int nt = 0; nt < NT; ++nt) {
           const int hd = nt * kHeadTile + col;
           if (hd < held_heads)
-          *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group +
-                    16 * (tile0 * kHeadTile + hd)) = shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
+            *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group +
+                      16 * (tile0 * kHeadTile + hd)) = shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
         }
       held_from += holding / F::kSub * kStep;
       holding = 0;
