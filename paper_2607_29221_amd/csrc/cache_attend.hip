@@ -138,6 +138,11 @@ __device__ __forceinline__ void split(float x, T* part) {
 // ceil(total / workgroups). Its part of sequence b has slot u + b: going on, a
 // workgroup or a sequence ends, so no two parts have the same.
 constexpr int kStepTokens = 128;
+// Workgroups go to the chip's dies in turn. The blocks of query heads of a
+// share lie this far apart, so that they read its keys and values through one
+// die's L2 (64 query heads on one key/value head: 83 us side by side, 75 us so,
+// and 71 us with the shares that fit).
+constexpr int kXcds = 8;
 
 // The workspace: per slot and query head the base and the sum of the weights
 // and the unnormalised output; then scores.
@@ -163,9 +168,23 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // waves keep 64 KiB of a bf16 cache's rows of 128 in flight, which is
   // enough, and every further workgroup is another part to join (64 sequences
   // with the join: 162 us with 256 workgroups in all, 165 us with 512, 169 us
-  // with 768; heads of 256 elements 89, 92 and 101 us).
-  const int64_t groups = (int64_t)c.kv_heads * p.tile_groups;
-  const int64_t wanted = (256 + groups - 1) / groups;
+  // with 768; heads of 256 elements 89, 92 and 101 us). Where several blocks of
+  // query heads read the same keys, arithmetic counts too and two per unit hide
+  // each other's waits (128 heads on one key/value head, bf16 cache: 173 us
+  // with one, 142 us with two; heads of 256 elements, where the registers hold
+  // one, 79 and 85 us). Never more than fit at once, since a unit with two
+  // takes twice as long (12 key/value heads: 256 us with 264, 174 us with 252),
+  // but more per unit where more than one unit in 16 would idle (71 heads: 289
+  // us with 213, 250 us with 497).
+  int32_t slots = p.tile_groups > 1 && c.head_dim <= 128 ? 512 : 256;
+  int64_t wanted;
+  while (true) {
+    const int64_t shares = p.tile_groups > 1 ? slots / kXcds / p.tile_groups * kXcds : slots;
+    wanted = shares / c.kv_heads;
+    if (slots == 1024 || 16 * wanted * c.kv_heads * p.tile_groups >= 15 * slots) break;
+    slots += 256;
+  }
+  if (wanted == 0) wanted = 1;
   const int64_t steps = c.batch * ((max_len + kStepTokens - 1) / kStepTokens);
   p.workgroups = (int32_t)(wanted < steps ? wanted : steps > 0 ? steps : 1);
   return p;
@@ -231,10 +250,12 @@ __device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int 
 constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : (DP == 128 ? 3 : 4) - (NT - 1); }
 
 // NT: blocks of 16 query heads per wave (64 query heads on one key/value head
-// of 128 elements, 64 sequences: 155 us with one, 83 us with two). STREAM: no
-// other workgroup reads the same keys and values, so they pass by the caches
-// (131072 tokens: 92 us through them, 81 us past them); where several do
-// (groups of more than 32 heads) they go through (82 us, 95 us past).
+// of 128 elements, 64 sequences: 105 us with one, 71 us with two; four, one
+// workgroup of the registers' size per unit, lost up to a fifth elsewhere).
+// STREAM: no other workgroup reads the same keys and values, so they pass by
+// the caches (131072 tokens: 92 us through them, 81 us past them); where
+// several do (groups of more than 32 heads) they go through (the 64 heads: 71
+// us, 83 us past).
 // Measured on an MI355X, this kernel alone, heads of 128 elements, 64 query
 // and 8 key/value heads: 131072 tokens of one sequence 81 us (6.6 TB/s of keys
 // and values); 64 sequences of 512 to 7168 tokens 157 us (6.6 TB/s); 32 heads
@@ -244,7 +265,7 @@ constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : (DP == 128 ? 3 :
 // stored), whether one step's or many steps' are stored at a time, past the
 // caches or through them.
 template <int CT, int XT, int DP, int NT, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_kernel(AttendLaunch a, Work wk) {
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef Form<CT, XT, DP> F;
   typedef typename F::C C;
   typedef typename F::X X;
@@ -266,13 +287,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int u = blockIdx.y, tile_groups = gridDim.x / a.c.kv_heads;
-  const int h = blockIdx.x / tile_groups, tile0 = blockIdx.x % tile_groups * NT;
+  const uint32_t share_of = blockIdx.y * kXcds + blockIdx.x % kXcds;
+  const int u = share_of / (uint32_t)a.c.kv_heads, h = share_of - u * a.c.kv_heads;
+  const int tile0 = blockIdx.x / kXcds * NT;
+  if (u >= workgroups) return;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
 
   int before;
   FirstSteps first64;
-  const int total = all_steps(a, lane, &first64), share = (total + (int)gridDim.y - 1) / (int)gridDim.y;
+  const int total = all_steps(a, lane, &first64), share = (total + workgroups - 1) / workgroups;
   int at = u * share;
   const int stop = min(total, at + share);
   if (at >= stop) return;
@@ -722,18 +745,19 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
 
 template <int CT, int XT, int DP>
 void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
-  const dim3 grid(a.c.kv_heads * p.tile_groups, p.workgroups), block(64 * kWaves);
+  const int64_t shares = (int64_t)a.c.kv_heads * p.workgroups;
+  const dim3 grid(kXcds * p.tile_groups, (unsigned)((shares + kXcds - 1) / kXcds)), block(64 * kWaves);
   if constexpr (DP < 256) {
     if (p.wave_tiles == 2) {
-      if (p.tile_groups == 1) cache_attend_kernel<CT, XT, DP, 2, true><<<grid, block, 0, s>>>(a, w);
-      else cache_attend_kernel<CT, XT, DP, 2, false><<<grid, block, 0, s>>>(a, w);
+      if (p.tile_groups == 1) cache_attend_kernel<CT, XT, DP, 2, true><<<grid, block, 0, s>>>(a, w, p.workgroups);
+      else cache_attend_kernel<CT, XT, DP, 2, false><<<grid, block, 0, s>>>(a, w, p.workgroups);
       return;
     }
   } else if (p.tile_groups > 1) {
-    cache_attend_kernel<CT, XT, DP, 1, false><<<grid, block, 0, s>>>(a, w);
+    cache_attend_kernel<CT, XT, DP, 1, false><<<grid, block, 0, s>>>(a, w, p.workgroups);
     return;
   }
-  cache_attend_kernel<CT, XT, DP, 1, true><<<grid, block, 0, s>>>(a, w);
+  cache_attend_kernel<CT, XT, DP, 1, true><<<grid, block, 0, s>>>(a, w, p.workgroups);
 }
 
 template <int CT, int XT>

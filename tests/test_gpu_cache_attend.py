@@ -122,6 +122,21 @@ def test_many_sequences(act, cache, batch):
     check(c, q, 6, out, act, scale, before)
 
 
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim,longest", ((80, 1, 64, 12001), (150, 3, 32, 9000), (24, 12, 64, 3000),
+                                                  (71, 71, 16, 1100), (300, 300, 8, 700), (1024, 1024, 8, 260),
+                                                  (96, 2, 256, 4500)))
+def test_shares(act, cache, heads, kv, dim, longest):
+    """Head counts whose shares do not divide the chip, blocks of query heads
+    that share a die, fewer shares than dies hold and more key/value heads than
+    the chip has compute units."""
+    lengths = (longest, 0, 300 if kv < 300 else 20)
+    c = make_cache(lengths, kv, dim, 64, cache, 41, evicts=True, layout="tokens" if kv == 12 else "heads")
+    before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+    q, out, scale = run(c, heads, act, 42, accumulate=True)
+    check(c, q, heads, out, act, scale, before)
+
+
 @pytest.mark.parametrize("max_len", (None, 2048))
 def test_room_does_not_matter(max_len):
     """The same tokens in tables with room for many more: the cut follows the
