@@ -171,7 +171,7 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // with 768; heads of 256 elements 89, 92 and 101 us). Where several blocks of
   // query heads read the same keys, arithmetic counts too and two per unit hide
   // each other's waits (128 heads on one key/value head, bf16 cache: 173 us
-  // with one, 142 us with two; heads of 256 elements, where the registers hold
+  // with one, 130 to 142 us with two; heads of 256 elements, where the registers hold
   // one, 79 and 85 us). Never more than fit at once, since a unit with two
   // takes twice as long (12 key/value heads: 256 us with 264, 174 us with 252),
   // but more per unit where more than one unit in 16 would idle (71 heads: 289
@@ -250,8 +250,9 @@ __device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int 
 constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : (DP == 128 ? 3 : 4) - (NT - 1); }
 
 // NT: blocks of 16 query heads per wave (64 query heads on one key/value head
-// of 128 elements, 64 sequences: 105 us with one, 71 us with two; four, one
-// workgroup of the registers' size per unit, lost up to a fifth elsewhere).
+// of 128 elements, 64 sequences: 105 us with one, 71 us with two; four
+// leave the registers one wave per SIMD and took up to a fifth longer with
+// float32 activations).
 // STREAM: no other workgroup reads the same keys and values, so they pass by
 // the caches (131072 tokens: 92 us through them, 81 us past them); where
 // several do (groups of more than 32 heads) they go through (the 64 heads: 71
