@@ -36,7 +36,8 @@
  * A block-table entry outside [0, pages) is a page that is not there: its
  * tokens are not read, not written and not evicted to. Sequences share no
  * page that a call writes to (through append, accumulated weights or
- * eviction).
+ * eviction). ``ldt`` 0 is one row of the table that all sequences share; only
+ * attention without accumulated weights takes it.
  *
  * ``state`` is an int32 array [2][batch]: the number of tokens that sequence
  * b holds (a negative one counts as 0, and one beyond the block table's
@@ -95,7 +96,8 @@ typedef struct mosaic_rotary {
   const int32_t* positions;   /* naxes x ldp, a token's place on every axis
                                  (one outside the table counts as its nearest
                                  row); NULL: its number in its sequence */
-  int64_t ldp;
+  int64_t ldp;                /* at least the tokens, or 0: all axes share one
+                                 row of places */
   int32_t naxes;              /* 1 to 4 */
   int32_t sections[4];
   int32_t interleaved;

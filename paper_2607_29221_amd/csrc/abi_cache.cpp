@@ -49,7 +49,7 @@ mosaic_status view_of(const mosaic_kv_cache* c, CacheView* v) {
     return fail(MOSAIC_ERR_INVALID_ARG, "pages overlap");
   if (c->batch > 0 && c->max_blocks > 0) {
     if (c->block_table == nullptr) return fail(MOSAIC_ERR_INVALID_ARG, "block_table is NULL");
-    if (c->ldt < c->max_blocks) return fail(MOSAIC_ERR_INVALID_ARG, "ldt < max_blocks");
+    if (c->ldt != 0 && c->ldt < c->max_blocks) return fail(MOSAIC_ERR_INVALID_ARG, "ldt < max_blocks");
   }
   if (c->pages > 0 && (c->k == nullptr || c->v == nullptr)) return fail(MOSAIC_ERR_INVALID_ARG, "k or v is NULL");
   if (!aligned16(c->k) || !aligned16(c->v)) return fail(MOSAIC_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
@@ -69,6 +69,13 @@ mosaic_status view_of(const mosaic_kv_cache* c, CacheView* v) {
   v->head_dim = c->head_dim;
   v->log2_page = __builtin_ctz((unsigned)c->page_size);
   v->dtype = c->dtype;
+  return MOSAIC_OK;
+}
+
+// Calls that write to pages: not to those of a table that all sequences share.
+mosaic_status check_own_pages(const CacheView& v) {
+  if (v.batch > 1 && v.max_blocks > 0 && v.ldt == 0)
+    return fail(MOSAIC_ERR_INVALID_ARG, "sequences that share their block table cannot be written to");
   return MOSAIC_OK;
 }
 
@@ -116,6 +123,8 @@ mosaic_status check_attend(const mosaic_kv_cache* cache, int32_t heads, int64_t 
   if (heads < 1 || heads % a->c.kv_heads != 0)
     return fail(MOSAIC_ERR_INVALID_ARG, "%d query heads are no multiple of %d key/value heads", heads, a->c.kv_heads);
   if (heads > 4096) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 4096 query heads");
+  const mosaic_status own = accumulate != 0 ? check_own_pages(a->c) : MOSAIC_OK;
+  if (own != MOSAIC_OK) return own;
   a->heads = heads;
   a->max_len = max_len < slots_of(a->c) ? max_len : slots_of(a->c);
   a->accumulate = accumulate != 0;
@@ -125,8 +134,8 @@ mosaic_status check_attend(const mosaic_kv_cache* cache, int32_t heads, int64_t 
 }
 
 mosaic_status check_evict(const mosaic_kv_cache* cache, int64_t max_len, int64_t budget, EvictLaunch* a) {
-  const mosaic_status st = view_of(cache, &a->c);
-  if (st != MOSAIC_OK) return st;
+  mosaic_status st = view_of(cache, &a->c);
+  if (st != MOSAIC_OK || (st = check_own_pages(a->c)) != MOSAIC_OK) return st;
   if (max_len < 0 || budget < 1) return fail(MOSAIC_ERR_INVALID_ARG, "negative max_len, or a budget below 1");
   a->max_len = max_len < slots_of(a->c) ? max_len : slots_of(a->c);
   a->budget = budget;
@@ -142,7 +151,7 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
                                   void* q_out, int64_t ldq, const int32_t* state, int32_t* new_state, void* stream) {
   AppendLaunch a{};
   mosaic_status st = view_of(cache, &a.c);
-  if (st != MOSAIC_OK) return st;
+  if (st != MOSAIC_OK || (st = check_own_pages(a.c)) != MOSAIC_OK) return st;
   if ((st = check_heads(a.c, heads, x_dtype)) != MOSAIC_OK) return st;
   if (rows < 0) return fail(MOSAIC_ERR_INVALID_ARG, "negative size");
   if (rows > (1 << 22)) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^22 tokens");
@@ -167,7 +176,8 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
       return fail(MOSAIC_ERR_INVALID_ARG, "%lld pairs in heads of %lld", (long long)pairs, (long long)D);
     if (rotary->table == nullptr || rotary->rows < 1) return fail(MOSAIC_ERR_INVALID_ARG, "rotary table is NULL or empty");
     if (rotary->rows > INT32_MAX) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^31 - 1 rows of the rotary table");
-    if (rotary->positions != nullptr && rotary->ldp < rows) return fail(MOSAIC_ERR_INVALID_ARG, "ldp < rows");
+    if (rotary->positions != nullptr && rotary->ldp != 0 && rotary->ldp < rows)
+      return fail(MOSAIC_ERR_INVALID_ARG, "ldp < rows");
     a.rot.table = rotary->table;
     a.rot.rows = rotary->rows;
     a.rot.positions = rotary->positions;

@@ -521,7 +521,7 @@ struct Cache {
     c.page_stride = k->stride(0);
     c.head_stride = k->stride(1);
     c.token_stride = k->stride(2);
-    c.ldt = t->stride(0) > t->size(1) ? t->stride(0) : t->size(1);
+    c.ldt = t->size(0) > 1 ? t->stride(0) : t->size(1);   // a single row's stride has no meaning
     if (!state_like(st) || (w != nullptr && !numbers(w, at::kFloat)) || (r != nullptr && !numbers(r, at::kInt))) return false;
     c.k = k->data_ptr();
     c.v = v->data_ptr();
@@ -600,7 +600,7 @@ FUNCTION(cache_append, 7) {
       NEED(positions->scalar_type() == at::kInt && positions->size(0) >= axes && positions->size(1) >= rows &&
            positions->stride(1) == 1);
       r.positions = (const int32_t*)positions->data_ptr();
-      r.ldp = positions->stride(0) > rows ? positions->stride(0) : rows;
+      r.ldp = axes > 1 ? positions->stride(0) : rows;
     }
     r.table = (const float*)table->data_ptr();
     r.rows = table->size(0);

@@ -613,8 +613,9 @@ def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
             if t.shape != k.shape[:3] or not t.is_contiguous():
                 raise ValueError(f"cache.{name} must be a contiguous (pages, kv_heads, page_size) tensor")
     pages, heads, page, dim = k.shape
+    # a single row's stride has no meaning; 0 is a table that all sequences share
     return _lib.MosaicKvCache(k=_ptr(k), v=_ptr(v), weights=_ptr(cache.weights), order=_ptr(cache.order),
-                              block_table=_ptr(table), ldt=max(table.stride(0), blocks), pages=pages,
+                              block_table=_ptr(table), ldt=table.stride(0) if batch > 1 else blocks, pages=pages,
                               page_stride=k.stride(0), head_stride=k.stride(1), token_stride=k.stride(2),
                               dtype=_FTYPE[k.dtype], batch=batch, max_blocks=blocks, kv_heads=heads, head_dim=dim,
                               page_size=page)
@@ -673,8 +674,9 @@ def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: to
             if rotary.positions.shape[0] < len(sections) or rotary.positions.shape[1] < rows or \
                     rotary.positions.stride(1) != 1:
                 raise ValueError("rotary.positions must hold a row of places for every axis")
-        r = _lib.MosaicRotary(table=_ptr(rotary.table), rows=rotary.table.shape[0], positions=_ptr(rotary.positions),
-                              ldp=0 if rotary.positions is None else max(rotary.positions.stride(0), rows),
+        # 0: places that all axes share
+        ldp = 0 if rotary.positions is None else rotary.positions.stride(0) if len(sections) > 1 else rows
+        r = _lib.MosaicRotary(table=_ptr(rotary.table), rows=rotary.table.shape[0], positions=_ptr(rotary.positions), ldp=ldp,
                               naxes=len(sections), sections=(ctypes.c_int32 * 4)(*sections),
                               interleaved=1 if rotary.interleaved else 0)
     _check(_lib.load().mosaic_cache_append(ctypes.byref(c), _ptr(qkv), qkv.stride(0), _FTYPE[qkv.dtype], rows,
