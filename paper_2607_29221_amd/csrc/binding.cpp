@@ -598,7 +598,7 @@ FUNCTION(cache_append, 7) {
     NEED(ok);
     if (positions != nullptr) {
       NEED(positions->scalar_type() == at::kInt && positions->size(0) >= axes && positions->size(1) >= rows &&
-           positions->stride(1) == 1);
+           (rows == 1 || positions->stride(1) == 1));
       r.positions = (const int32_t*)positions->data_ptr();
       r.ldp = axes > 1 ? positions->stride(0) : rows;
     }

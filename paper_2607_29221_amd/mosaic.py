@@ -672,7 +672,7 @@ def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: to
         if rotary.positions is not None:
             _device_tensor(rotary.positions, "rotary.positions", _INT, 2)
             if rotary.positions.shape[0] < len(sections) or rotary.positions.shape[1] < rows or \
-                    rotary.positions.stride(1) != 1:
+                    (rows > 1 and rotary.positions.stride(1) != 1):
                 raise ValueError("rotary.positions must hold a row of places for every axis")
         # 0: places that all axes share
         ldp = 0 if rotary.positions is None else rotary.positions.stride(0) if len(sections) > 1 else rows

@@ -163,3 +163,44 @@ def test_rows_that_overlap_are_refused(monkeypatch, native):
     with pytest.raises(m.MosaicError) as e:
         m.mosaic_cache_append(c, torch.zeros((3, 512), device="cuda"), 4, q, rotary=rotary)
     assert e.value.status == m.STATUS_INVALID_ARG
+
+
+def test_places_of_one_token_have_no_stride(monkeypatch):
+    """A token's places as a column: between its only entry and the next lies
+    nothing that is read."""
+    rec = _Recorder()
+    monkeypatch.setattr(m, "_b", rec)
+    monkeypatch.setattr(m._lib, "load", lambda: rec)
+    monkeypatch.setattr(m, "_stream", lambda: 0)
+    monkeypatch.setattr(m, "_device_tensor", lambda *args: None)
+    c = m.KVCache.empty(1, 40, 2, 64, page_size=16, device="cpu")
+    places = torch.zeros((1, 3), dtype=torch.int32).t()
+    assert places.stride() == (1, 3)
+    m.mosaic_cache_append(c, torch.zeros(1, 512), 4, torch.zeros(1, 256),
+                          rotary=m.Rotary(m.Rotary.frequencies(16, 6, device="cpu"), [2, 2, 2], places))
+    assert rec.ldp == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", (True, False))
+def test_places_of_one_token_as_a_column(monkeypatch, native):
+    _ways(monkeypatch, native)
+    old = make_cache((7,), 2, 64, 16, "bf16", 35, room=2)
+    x = torch.randn((1, 512), generator=seeded(36), device="cuda")
+    column = torch.tensor([[3, 11, 29]], dtype=torch.int32, device="cuda").t()
+    got = []
+    for places in (column, column.contiguous()):
+        c, q = clone(old), torch.empty((1, 256), device="cuda")
+        m.mosaic_cache_append(c, x, 4, q, rotary=m.Rotary(m.Rotary.frequencies(32, 32), [8, 12, 12], places))
+        got.append((q, c.k, c.v))
+    assert all(same_bits(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.gpu
+def test_native_takes_places_of_one_token_as_a_column():
+    c = make_cache((7,), 2, 64, 16, "bf16", 45, room=2)
+    rotary = m.Rotary(m.Rotary.frequencies(32, 32), [8, 12, 12],
+                      torch.tensor([[3, 11, 29]], dtype=torch.int32, device="cuda").t())
+    x, q = torch.zeros((1, 512), device="cuda"), torch.zeros((1, 256), device="cuda")
+    assert m._native().cache_append(c, x, 4, q, None, rotary, None) == 0
+    torch.cuda.synchronize()
