@@ -46,9 +46,32 @@ PyObject *s_k, *s_v, *s_block_table, *s_state, *s_weights, *s_order, *s_table, *
 PyObject *get_device, *get_stream;                                               // torch._C functions
 PyObject* rng_type;                                                              // the ctypes struct of mosaic_rng
 
+// An object held until the function returns: what an attribute gives may
+// belong to nobody else (a property that makes a view), or be replaced by
+// another thread while the call runs without the interpreter lock.
+class Ref {
+ public:
+  Ref() = default;
+  Ref(const Ref&) = delete;
+  Ref& operator=(const Ref&) = delete;
+  ~Ref() { Py_XDECREF(o_); }
+  PyObject* take(PyObject* o) {      // a new reference, or null
+    Py_XDECREF(o_);
+    return o_ = o;
+  }
+  PyObject* hold(PyObject* o) {      // a borrowed one
+    Py_XINCREF(o);
+    return take(o);
+  }
+
+ private:
+  PyObject* o_ = nullptr;
+};
+
 struct Mat {
   void* p = nullptr;
   int64_t ld = 0;
+  Ref buf;                           // of a Digits view
   bool given() const { return p != nullptr; }
 };
 
@@ -83,7 +106,7 @@ bool vec(PyObject* o, int64_t n, at::ScalarType dt, bool optional, Mat* m) {
 // A Digits view that holds rows x cols, or None if optional.
 bool digits(PyObject* o, int64_t rows, int64_t cols, bool optional, Mat* m) {
   if (o == Py_None) return optional;
-  PyObject* b = PyObject_GetAttr(o, s_buf);
+  PyObject* b = m->buf.take(PyObject_GetAttr(o, s_buf));
   PyObject* c = b != nullptr ? PyObject_GetAttr(o, s_col0) : nullptr;
   bool ok = false;
   if (c != nullptr && PyLong_CheckExact(c)) {
@@ -96,7 +119,6 @@ bool digits(PyObject* o, int64_t rows, int64_t cols, bool optional, Mat* m) {
       ok = t->data_ptr() != nullptr;
     }
   }
-  Py_XDECREF(b);     // its owner keeps the tensor
   Py_XDECREF(c);
   PyErr_Clear();
   return ok;
@@ -162,7 +184,7 @@ bool truth(PyObject* o, int32_t* v) {
 
 // The status of an ABI call, made without the interpreter lock: a launch may
 // wait for room in its stream's queue, and other threads go on meanwhile (the
-// caller's frame holds the arguments).
+// caller's frame holds the arguments, a Ref what was got from them).
 template <class Call>
 PyObject* status(Call call) {
   int32_t st;
@@ -376,8 +398,9 @@ FUNCTION(stream_terms, 5) {
   const Py_ssize_t n = PyList_GET_SIZE(a[0]);
   NEED(n >= 1 && n <= kMaxTerms);
   mosaic_stream_term terms[kMaxTerms];
+  Ref tuples[kMaxTerms];
   for (Py_ssize_t l = 0; l < n; ++l) {
-    PyObject* t = PyList_GET_ITEM(a[0], l);
+    PyObject* t = tuples[l].hold(PyList_GET_ITEM(a[0], l));
     Rng r;
     Mat d;
     int64_t rcols;
@@ -391,13 +414,12 @@ FUNCTION(stream_terms, 5) {
   });
 }
 
-bool attr_ptr(PyObject* o, PyObject* name, at::ScalarType dt, const void** p, int64_t* n = nullptr) {
-  PyObject* v = PyObject_GetAttr(o, name);
+bool attr_ptr(PyObject* o, PyObject* name, at::ScalarType dt, Ref* held, const void** p, int64_t* n = nullptr) {
+  PyObject* v = held->take(PyObject_GetAttr(o, name));
   const at::Tensor* t = v != nullptr ? plain(v) : nullptr;
   const bool ok = t != nullptr && t->dim() == 1 && t->scalar_type() == dt && t->stride(0) == 1;
   if (ok) *p = t->data_ptr();
   if (ok && n != nullptr) *n = t->size(0);
-  Py_XDECREF(v);
   PyErr_Clear();
   return ok && *p != nullptr;
 }
@@ -420,8 +442,9 @@ FUNCTION(cols_terms, 8) {
   const Py_ssize_t n = PyList_GET_SIZE(a[0]);
   NEED(n >= 1 && n <= kMaxTerms);
   mosaic_sparse_term terms[kMaxTerms];
+  Ref tuples[kMaxTerms], arrays[kMaxTerms][3];
   for (Py_ssize_t l = 0; l < n; ++l) {
-    PyObject* t = PyList_GET_ITEM(a[0], l);
+    PyObject* t = tuples[l].hold(PyList_GET_ITEM(a[0], l));
     NEED(PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 2);
     PyObject* p = PyTuple_GET_ITEM(t, 0);
     int64_t rows, cols, capacity = 0;
@@ -429,8 +452,8 @@ FUNCTION(cols_terms, 8) {
     Mat d;
     NEED(attr_size(p, s_rows, &rows) && attr_size(p, s_cols, &cols) && (l == 0 || rows == N));
     N = rows;
-    NEED(attr_ptr(p, s_row_ptr, at::kLong, &rp) && attr_ptr(p, s_col_idx, at::kInt, &ci) &&
-         attr_ptr(p, s_values, at::kInt, &va, &capacity) && matrix(PyTuple_GET_ITEM(t, 1), M, cols, at::kInt, false, &d));
+    NEED(attr_ptr(p, s_row_ptr, at::kLong, &arrays[l][0], &rp) && attr_ptr(p, s_col_idx, at::kInt, &arrays[l][1], &ci) &&
+         attr_ptr(p, s_values, at::kInt, &arrays[l][2], &va, &capacity) && matrix(PyTuple_GET_ITEM(t, 1), M, cols, at::kInt, false, &d));
     terms[l] = mosaic_sparse_term{(const int64_t*)rp, (const int32_t*)ci, (const uint32_t*)va, cols,
                                   (const uint32_t*)d.p, d.ld};
     all_cols += cols;
@@ -464,17 +487,16 @@ FUNCTION(cols_terms, 8) {
 // ---------------------------------------------------------------------------
 // Cached decoding
 
-// An attribute that is a plain tensor of dtype dt and dim dimensions; null
-// otherwise (`none` tells None apart). Its owner keeps the tensor.
-const at::Tensor* attr(PyObject* o, PyObject* name, int64_t dim, bool* none = nullptr) {
-  PyObject* v = PyObject_GetAttr(o, name);
+// An attribute that is a plain tensor of dim dimensions; null otherwise
+// (`none` tells None apart).
+const at::Tensor* attr(PyObject* o, PyObject* name, int64_t dim, Ref* held, bool* none = nullptr) {
+  PyObject* v = held->take(PyObject_GetAttr(o, name));
   if (v == nullptr) {
     PyErr_Clear();
     return nullptr;
   }
   if (none != nullptr) *none = v == Py_None;
   const at::Tensor* t = v != Py_None ? plain(v) : nullptr;
-  Py_DECREF(v);
   return t != nullptr && t->dim() == dim ? t : nullptr;
 }
 
@@ -488,6 +510,7 @@ struct Cache {
   at::Device device = at::kCPU;
   int64_t slots;
   int32_t* state;
+  Ref held[6];
 
   // weights and order: the cache's or, by `like`, an argument's
   bool numbers(const at::Tensor* t, at::ScalarType dt) const {
@@ -498,9 +521,10 @@ struct Cache {
     return t->scalar_type() == at::kInt && t->dim() == 2 && t->size(0) == 2 && t->size(1) == c.batch && t->is_contiguous();
   }
   bool get(PyObject* o) {
-    const at::Tensor *k = attr(o, s_k, 4), *v = attr(o, s_v, 4), *t = attr(o, s_block_table, 2), *st = attr(o, s_state, 2);
+    const at::Tensor *k = attr(o, s_k, 4, &held[0]), *v = attr(o, s_v, 4, &held[1]);
+    const at::Tensor *t = attr(o, s_block_table, 2, &held[2]), *st = attr(o, s_state, 2, &held[3]);
     bool no_weights = false, no_order = false;
-    const at::Tensor *w = attr(o, s_weights, 3, &no_weights), *r = attr(o, s_order, 3, &no_order);
+    const at::Tensor *w = attr(o, s_weights, 3, &held[4], &no_weights), *r = attr(o, s_order, 3, &held[5], &no_order);
     if (k == nullptr || v == nullptr || t == nullptr || st == nullptr) return false;
     if ((w == nullptr && !no_weights) || (r == nullptr && !no_order)) return false;
     c = mosaic_kv_cache{};
@@ -572,9 +596,10 @@ FUNCTION(cache_append, 7) {
     NEED(t != nullptr && t->dim() == 1 && t->size(0) == cache.c.batch + 1 && vec(a[4], cache.c.batch + 1, at::kInt, false, &starts));
   }
   mosaic_rotary r{};
+  Ref held[2];
   if (a[5] != Py_None) {
     bool none = false;
-    const at::Tensor *table = attr(a[5], s_table, 2), *positions = attr(a[5], s_positions, 2, &none);
+    const at::Tensor *table = attr(a[5], s_table, 2, &held[0]), *positions = attr(a[5], s_positions, 2, &held[1], &none);
     NEED(table != nullptr && table->scalar_type() == at::kFloat && table->is_contiguous() && table->size(0) > 0);
     NEED(positions != nullptr || none);
     PyObject* sections = PyObject_GetAttr(a[5], s_sections);
