@@ -143,7 +143,9 @@ mosaic_status mosaic_cache_attend(const mosaic_kv_cache* cache, const void* q, i
  * ``budget`` of them, for each key/value head by itself: first those of the
  * ``recent`` latest that its sequence has seen (order >= seen - recent), then
  * those of the largest weight (a NaN comes after every number), ties going to
- * the lowest slot. Survivors in slots below the budget stay where they are;
+ * the lowest slot. A slot below the budget whose page is not there can hold
+ * none of them: as many fewer are kept, and the slot counts on as one in use
+ * that holds nothing. Survivors in slots below the budget stay where they are;
  * the others, in the order of their slots, go to the slots below the budget
  * that came free, in theirs, with their weight and order. Pages from
  * ceil(budget / page_size) on then hold nothing. Weights and order of all
@@ -151,7 +153,7 @@ mosaic_status mosaic_cache_attend(const mosaic_kv_cache* cache, const void* q, i
  * cache's own arrays (then the survivors that stay are not rewritten) and may
  * not overlap them otherwise; new_state = (min(n, budget), seen). ``kept``
  * (batch x kv_heads x budget, or NULL) gets for every slot the slot that its
- * token had before, -1 for a slot without one. 1 <= budget, 0 <= recent <=
+ * token had before, -1 for a slot without one or without a page. 1 <= budget, 0 <= recent <=
  * budget; the cache has weights and order. workspace 16-byte aligned. */
 mosaic_status mosaic_cache_evict_workspace(const mosaic_kv_cache* cache, int64_t max_len, int64_t budget,
                                            int64_t* bytes);

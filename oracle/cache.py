@@ -36,18 +36,21 @@ def attend(q, k, v, scale):
     return p @ v, p
 
 
-def evict(weights, order, seen, budget, recent):
+def evict(weights, order, seen, budget, recent, there=None):
     """The slot that the token of each slot had before: weights and order by
-    slot, of all the tokens held."""
+    slot, of all the tokens held. ``there``: which slots have a page (None:
+    all); -1 for one that does not."""
     n = len(weights)
+    there = [True] * n if there is None else list(there)
     if n <= budget:
-        return list(range(n))
+        return [i if there[i] else -1 for i in range(n)]
     def rank(i):
         w = float(weights[i])
         if order[i] >= seen - recent:
             return (0, 0.0, i)
         return (2, 0.0, i) if np.isnan(w) else (1, -w, i)
-    stay = sorted(sorted(range(n), key=rank)[:budget])
+    room = [i for i in range(budget) if there[i]]
+    stay = sorted(sorted((i for i in range(n) if there[i]), key=rank)[:len(room)])
     inside = {i for i in stay if i < budget}
     movers = iter(i for i in stay if i >= budget)
-    return [i if i in inside else next(movers) for i in range(budget)]
+    return [-1 if not there[i] else i if i in inside else next(movers) for i in range(budget)]

@@ -35,10 +35,15 @@ constexpr int kChunk = 8192, kChunkThreads = 1024, kChunkKeys = kChunk / kChunkT
 // (2049 to 2048 with 256 threads per head: 10 us, 26 us by digits).
 constexpr int kFew = 4;
 
-// Rank of a token; a larger key stays before a smaller one. The latest come
-// first, then weights as numbers (0 and -0 alike), then NaN, then slots whose
-// page is not there.
-constexpr uint32_t kLatest = 0xFFFFFFFFu, kNan = 1u, kAbsent = 0u;
+// Rank of a slot; a larger key stays before a smaller one. The latest tokens
+// come first, then weights as numbers (0 and -0 alike), then NaN. A slot whose
+// page is not there holds nothing. Below the budget nothing can be moved to it
+// either: it stays, before everything else, as one of the budget's slots, so
+// the tokens that are there have that many fewer (ties go to the lowest slot,
+// so slots below the budget with the largest key always stay). Beyond the budget it
+// goes first; the slots that are there are never fewer than what is left of the
+// budget, so none such is among the survivors.
+constexpr uint32_t kHole = 0xFFFFFFFFu, kLatest = 0xFFFFFFFEu, kNan = 1u, kAbsent = 0u;
 __device__ __forceinline__ uint32_t rank_key(float w, bool latest) {
   if (latest) return kLatest;
   if (w != w) return kNan;
@@ -128,13 +133,14 @@ __device__ __forceinline__ void find_digit(const uint32_t (&own)[BINS / THREADS]
 }
 
 // The numbers of a token that stays in its slot, to wherever they are wanted.
-__device__ __forceinline__ void stay(const EvictLaunch& a, int32_t* kept, bool apart, int64_t row, int32_t slot,
-                                     float w, int32_t o) {
+// there: the slot has a page; row: its place in the arrays, or -1 if nothing is to be written.
+__device__ __forceinline__ void stay(const EvictLaunch& a, int32_t* kept, bool apart, bool there, int64_t row,
+                                     int32_t slot, float w, int32_t o) {
   if (apart && row >= 0) {
     a.new_weights[row] = w;
     a.new_order[row] = o;
   }
-  if (kept != nullptr) kept[slot] = slot;
+  if (kept != nullptr) kept[slot] = there ? slot : -1;
 }
 
 // A workgroup's slots first + THREADS r + tid: keys, and what they come from.
@@ -164,7 +170,10 @@ __device__ __forceinline__ void load_tokens(const EvictLaunch& a, int b, int h, 
     t.o[r] = order[safe];
   }
 #pragma unroll
-  for (int r = 0; r < R; ++r) t.key[r] = t.row[r] >= 0 ? rank_key(t.w[r], t.o[r] >= latest) : kAbsent;
+  for (int r = 0; r < R; ++r) {
+    const bool below = first + THREADS * r + (int)threadIdx.x < a.budget;
+    t.key[r] = t.row[r] >= 0 ? rank_key(t.w[r], t.o[r] >= latest) : below ? kHole : kAbsent;
+  }
 }
 
 // Numbers the slots first .. of a workgroup, of which `above` lower ones have
@@ -217,7 +226,7 @@ __device__ __forceinline__ void number_slots(const EvictLaunch& a, int b, int h,
       if (!stays) {
         l.free_slots[i - rank] = i;
       } else {
-        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
+        stay(a, kept, apart, t.key[r] != kHole, t.row[r], i, t.w[r], t.o[r]);
       }
     } else if (stays) {
       l.movers[budget - 1 - rank] = i;
@@ -254,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
   if (n <= a.budget) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (THREADS * r + tid < n) stay(a, kept, apart, t.row[r], THREADS * r + tid, t.w[r], t.o[r]);
+      if (THREADS * r + tid < n) stay(a, kept, apart, t.row[r] >= 0, t.row[r], THREADS * r + tid, t.w[r], t.o[r]);
     return;
   }
   const int32_t budget = (int32_t)a.budget;
@@ -295,7 +304,7 @@ __global__ __launch_bounds__(THREADS) void cache_select_kernel(EvictLaunch a, in
       if (i >= n) continue;
       const bool stays = ((gone >> r) & 1u) == 0u;
       if (i < budget && stays) {
-        stay(a, kept, apart, t.row[r], i, t.w[r], t.o[r]);
+        stay(a, kept, apart, t.row[r] >= 0, t.row[r], i, t.w[r], t.o[r]);
       } else if (i < budget || stays) {
         int32_t lower = 0, lower_within = 0;      // evicted slots below i, and those within the budget
 #pragma unroll
@@ -428,7 +437,7 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
     for (int32_t i = first + tid; i < min(n, first + kNumberKeys * kChunkThreads); i += kChunkThreads) {
       const int32_t page = page_of(a.c, b, i);
       const int64_t row = page >= 0 ? row_index(a.c, page, h, i) : -1;
-      stay(a, kept, apart, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
+      stay(a, kept, apart, row >= 0, row, i, row >= 0 ? a.c.weights[row] : 0.0f, row >= 0 ? a.c.order[row] : 0);
     }
     return;
   }
@@ -516,8 +525,7 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
   for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {
     const int32_t m = w / chunks, c = w - m * chunks;
     const int32_t from = l.movers[all - 1 - (first + m)], to = l.free_slots[first + m];
-    const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);
-    if (pf < 0 || pt < 0) continue;
+    const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);   // both are there: see rank_key
     const int64_t of = row_offset(a.c, pf, h, from) + 16 * c, ot = row_offset(a.c, pt, h, to) + 16 * c;
     const u32x4 k = *(const u32x4*)(a.c.k + of), v = *(const u32x4*)(a.c.v + of);
     *(u32x4*)(a.c.k + ot) = k;
