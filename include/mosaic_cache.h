@@ -125,8 +125,9 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
  * kv_heads))
  *     p_i = exp(scale q_g . k_i) / sum_j exp(scale q_g . k_j),
  *     out_g = sum_i p_i v_i,
- * zeros for a sequence without tokens. Scores, softmax sums and outputs are
- * accumulated in float32. ``accumulate`` nonzero adds p_i of every head of
+ * zeros for a sequence without tokens. Infinities and NaN among the tokens act
+ * as in these formulas (a score of -inf is no weight; zeros if there is no
+ * other). Scores, softmax sums and outputs are accumulated in float32. ``accumulate`` nonzero adds p_i of every head of
  * the group to ``weights`` of slot i and head h (without atomics: two runs
  * give the same bits). q and out are batch x heads * head_dim of x_dtype
  * (MOSAIC_F32 or the cache's type), 16-byte aligned, ldq and ldo multiples of

@@ -26,13 +26,16 @@ def rotate(x, table, places, sections, interleaved):
 
 def attend(q, k, v, scale):
     """q (group x dim), k and v (tokens x dim): the outputs (group x dim) and
-    the attention weights (group x tokens); zeros without tokens."""
+    the attention weights (group x tokens); zeros without tokens of a score
+    above -inf."""
     q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
     if len(k) == 0:
         return np.zeros((len(q), v.shape[1])), np.zeros((len(q), 0))
     s = scale * (q @ k.T)
-    p = np.exp(s - s.max(axis=1, keepdims=True))
-    p /= p.sum(axis=1, keepdims=True)
+    top = s.max(axis=1, keepdims=True)
+    p = np.exp(s - np.where(top == -np.inf, 0.0, top))
+    total = p.sum(axis=1, keepdims=True)
+    p /= np.where(total == 0.0, 1.0, total)
     return p @ v, p
 
 

@@ -31,6 +31,9 @@
 //   workgroup takes part of one sequence or several. A second kernel joins the
 //   parts, and adds up attention weights from the scores that the first one
 //   left in the workspace.
+#include <cfloat>
+#include <type_traits>
+
 #include "cache.h"
 #include "device_common.h"
 #include "dispatch.h"
@@ -409,14 +412,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
           constexpr int PER = 16 / (int)sizeof(X);
           const Chunk<X> v = __builtin_bit_cast(Chunk<X>, raw[nt][c][e / PER]);
           x[c][e] = there ? (float)v.e[e % PER] : 0.0f;
-          top = fmaxf(top, fabsf(x[c][e]));
+          top = fmaxf(top, fminf(fabsf(x[c][e]), FLT_MAX));
         }
       }
       int up = 0;
       if (CT == MOSAIC_F16 && XT == MOSAIC_F32) {
         // by a power of two into the upper part of the range of f16
         top = head_max(top);
-        up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+        up = top > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
       }
       scale[nt] = ldexpf(a.scale_log2, -up);
 #pragma unroll
@@ -438,21 +441,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
 
     f32x4 acc[NT][NV][EV];
     float top[NT], base[NT], sum[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      top[nt] = -INFINITY;
-      base[nt] = sum[nt] = 0.0f;
-    }
 
     // Scores go to memory through LDS, many steps at a time: a load that is
     // issued behind a store waits for it, and stores take longer than loads.
     float* scores = wk.scores + ((int64_t)b * a.heads + h * group) * wk.row + 4 * quad;
     const int held_heads = min(group - tile0 * kHeadTile, NT * kHeadTile);
-    int holding = 0, held_from = first;           // blocks of 16 tokens, and the first one's step
+    int holding, held_from;                       // blocks of 16 tokens, and the first one's step
     auto release = [&]() {
       for (int k = 0; k < holding; ++k)
 #pragma unroll
@@ -466,102 +460,148 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
       holding = 0;
     };
 
-    for (int t = first; t < t1; t += kStep) {
-      asm volatile("" ::: "memory");              // the queries stay in LDS
-      Block next[F::kSub];
-#pragma unroll
-      for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
-
-      float p[NT][F::kRows], tile_top[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        f32x4 dot[F::kSub];
-#pragma unroll
-        for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part)           // small terms first
-#pragma unroll
-          for (int c = 0; c < KL; ++c) {
-            const Frag q = shared.in.query[nt][part][c][lane];
-#pragma unroll
-            for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
-          }
-        tile_top[nt] = -INFINITY;
-#pragma unroll
-        for (int s = 0; s < F::kSub; ++s)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * scale[nt] : -INFINITY;
-            tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
-          }
-      }
-      load_keys(next);
-      if (a.accumulate) {
-        if (4 * held_heads * (holding + F::kSub) > kHold) release();
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int s = 0; s < F::kSub; ++s) {
-            const int hd = nt * kHeadTile + col;
-            if (hd < held_heads)
-              shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
-                  f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
-          }
-        holding += F::kSub;
-      }
-
-      Frag pf[NT][WPARTS];
+    // All steps of the part. Where a key or query holds an infinity, its products
+    // with the parts of the other (small ones of either sign, and zeros) can add
+    // up to NaN although the sum is infinite: `careful` takes such a score from
+    // the first parts alone, which have the signs of the whole. That is a second
+    // pass, for waves that found NaN: no step of the first has a check for it.
+    auto pass = [&](auto careful) __attribute__((always_inline)) {
+      constexpr bool kCareful = decltype(careful)::value;
+      holding = 0;
+      held_from = first;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
-          const float now = fmaxf(top[nt], head_max(tile_top[nt]));
-          const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
-          const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - rescaled);
-          sum[nt] *= f;
 #pragma unroll
-          for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int j = 0; j < EV; ++j) acc[nt][v][j] *= f;
-          top[nt] = now;
-          base[nt] = rescaled;
-        }
-#pragma unroll
-        for (int i = 0; i < F::kRows; ++i) {
-          const float w = exp2_fast(p[nt][i] - base[nt]);
-          sum[nt] += w;
-          C part[WPARTS];
-          split<C, WPARTS>(w, part);
-#pragma unroll
-          for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
-        }
+          for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        top[nt] = -INFINITY;
+        base[nt] = sum[nt] = 0.0f;
       }
+      for (int t = first; t < t1; t += kStep) {
+        asm volatile("" ::: "memory");              // the queries stay in LDS
+        Block next[F::kSub];
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
 
+        float p[NT][F::kRows], tile_top[NT];
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+        for (int nt = 0; nt < NT; ++nt) {
+          f32x4 dot[F::kSub];
 #pragma unroll
-        for (int j = 0; j < EV; ++j) {
-          Frag vf;
-          if constexpr (F::kWide) {
+          for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
-          } else {
-            u32x4 w;
+          for (int part = PARTS - 1; part >= 0; --part)           // small terms first
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2],
-                                           j % 2 ? 0x07060302u : 0x05040100u);
-            vf = __builtin_bit_cast(Frag, w);
+            for (int c = 0; c < KL; ++c) {
+              const Frag q = shared.in.query[nt][part][c][lane];
+#pragma unroll
+              for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
+            }
+          if constexpr (kCareful) {
+            f32x4 first_part[F::kSub];
+#pragma unroll
+            for (int s = 0; s < F::kSub; ++s) first_part[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < KL; ++c)
+#pragma unroll
+              for (int s = 0; s < F::kSub; ++s)
+                first_part[s] = M::mul(key[s][c], shared.in.query[nt][0][c][lane], first_part[s]);
+#pragma unroll
+            for (int s = 0; s < F::kSub; ++s)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) dot[s][i] = dot[s][i] == dot[s][i] ? dot[s][i] : first_part[s][i];
+          }
+          tile_top[nt] = -INFINITY;
+#pragma unroll
+          for (int s = 0; s < F::kSub; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * scale[nt] : -INFINITY;
+              tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
+            }
+        }
+        load_keys(next);
+        if (a.accumulate) {
+          if (4 * held_heads * (holding + F::kSub) > kHold) release();
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int s = 0; s < F::kSub; ++s) {
+              const int hd = nt * kHeadTile + col;
+              if (hd < held_heads)
+                shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
+                    f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
+            }
+          holding += F::kSub;
+        }
+
+        Frag pf[NT][WPARTS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
+            const float now = fmaxf(top[nt], head_max(tile_top[nt]));
+            const float rescaled = now == -INFINITY ? 0.0f : now - F::kShift;
+            const float f = top[nt] == -INFINITY ? 0.0f : exp2_fast(base[nt] - rescaled);
+            sum[nt] *= f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+              for (int j = 0; j < EV; ++j) acc[nt][v][j] *= f;
+            top[nt] = now;
+            base[nt] = rescaled;
           }
 #pragma unroll
-          for (int part = WPARTS - 1; part >= 0; --part)
+          for (int i = 0; i < F::kRows; ++i) {
+            const float w = exp2_fast(p[nt][i] - base[nt]);
+            sum[nt] += w;
+            C part[WPARTS];
+            split<C, WPARTS>(w, part);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
+            for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
+          }
         }
+
 #pragma unroll
-      for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
-      load_values(cur);
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < EV; ++j) {
+            Frag vf;
+            if constexpr (F::kWide) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
+            } else {
+              u32x4 w;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2],
+                                             j % 2 ? 0x07060302u : 0x05040100u);
+              vf = __builtin_bit_cast(Frag, w);
+            }
+#pragma unroll
+            for (int part = WPARTS - 1; part >= 0; --part)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
+          }
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
+        load_values(cur);
+      }
+      if (a.accumulate) release();
+    };
+    pass(std::false_type());
+    if constexpr (PARTS > 1) {
+      bool nan = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) nan = nan || sum[nt] != sum[nt];
+      if (__any(nan)) {
+#pragma unroll
+        for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
+        load_keys(cur);
+        load_values(cur);
+        pass(std::true_type());
+      }
     }
-    if (a.accumulate) release();
 
     // join the waves
     asm volatile("" : "+v"(own_lane));

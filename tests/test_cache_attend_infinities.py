@@ -1,0 +1,145 @@
+"""Infinities and NaN in held keys and in queries: a score is what the sum of
+the products is, so -inf leaves a token without weight and the rest as it is.
+Finite outputs to the bound of test_gpu_cache_attend.py; the others alike."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as oc
+from paper_2607_29221_amd import mosaic as m
+from tests.cache_util import DT, TINY, TYPES, UNIT, clone, f64, get, make_cache, put, seeded
+
+U = 2.0 ** -24
+
+
+def test_oracle_with_infinities():
+    inf = math.inf
+    v = np.array([[1.0], [2.0], [4.0]])
+    out, p = oc.attend([[1.0, 2.0]], [[1.0, -inf], [0.0, 0.0], [0.0, 0.0]], v, 0.5)
+    assert p.tolist() == [[0.0, 0.5, 0.5]] and out.tolist() == [[3.0]]
+    out, p = oc.attend([[1.0, 2.0]], [[1.0, -inf]] * 3, v, 0.5)
+    assert not p.any() and not out.any()
+    with np.errstate(invalid="ignore"):
+        out, p = oc.attend([[1.0, 2.0]], [[1.0, inf], [0.0, 0.0], [0.0, 0.0]], v, 0.5)
+    assert np.isnan(out).all()
+
+
+def alike(got, want, tol):
+    """The same NaN and infinities, the rest within tol."""
+    assert np.array_equal(np.isnan(got), np.isnan(want)), (np.isnan(got).sum(), np.isnan(want).sum())
+    infinite = np.isinf(want)
+    assert np.array_equal(np.isinf(got), infinite) and np.array_equal(got[infinite], want[infinite])
+    finite = np.isfinite(want)
+    assert (np.abs(got - want)[finite] <= tol[finite]).all(), np.abs(got - want)[finite].max()
+
+
+def attend_and_check(c, q, heads, act, accumulate=True):
+    KV, D = c.k.shape[1], c.k.shape[3]
+    G, lengths = heads // KV, c.state[0].tolist()
+    before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+    out = torch.full_like(q, float("nan"))
+    m.mosaic_cache_attend(c, q, heads, out, accumulate=accumulate)
+    got, qs, scale = f64(out).reshape(-1, heads, D), f64(q).reshape(-1, heads, D), D ** -0.5
+    seen = [0, 0]
+    with np.errstate(invalid="ignore"):
+        for b, n in enumerate(lengths):
+            k, v = get(c, "k", b, n), get(c, "v", b, n)
+            for h in range(KV):
+                rows = qs[b, h * G: (h + 1) * G]
+                o, p = oc.attend(rows, k[h], v[h], scale)
+                S = scale * (np.abs(np.nan_to_num(rows, posinf=0.0, neginf=0.0)) @
+                             np.abs(np.nan_to_num(k[h], posinf=0.0, neginf=0.0)).T).max(axis=1, keepdims=True)
+                rel = (2 * (D + 4) * S + n + 16) * U
+                A = p @ np.abs(v[h])
+                tol = (rel + (UNIT[act] if act != "f32" else 0.0)) * A + UNIT[act] * np.abs(o) + TINY[act]
+                alike(got[b, h * G: (h + 1) * G], o, tol)
+                add = p.sum(axis=0)
+                alike(get(c, "weights", b, n)[h], before[b][h] + add,
+                      (rel * p).sum(axis=0) + 4 * U * (before[b][h] + add) + 1e-38)
+                seen[0] += np.isfinite(o).all(axis=1).sum()
+                seen[1] += np.isnan(o).all(axis=1).sum()
+    return seen
+
+
+SHAPES = ((4, 2, 64), (8, 1, 128), (40, 2, 80), (3, 3, 256), (6, 2, 8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+def test_infinite_keys(act, cache, heads, kv, dim):
+    """One infinite element of some tokens' keys, against which every query has
+    the same sign: scores of -inf only, and every output is finite; then of
+    either sign, so that some heads' scores are inf."""
+    lengths = (1, 33, 700, 3000)
+    c = make_cache(lengths, kv, dim, 16, cache, 5, evicts=True)
+    q = torch.randn((4, heads, dim), generator=seeded(6), device="cuda")
+    q[:, :, 3] = q[:, :, 3].abs() + 0.1
+    q[:, 0, 3] = 1.0                                # nothing is left for further parts of it
+    q = q.reshape(4, heads * dim).to(DT[act])
+    r = np.random.default_rng(7)
+    for b, n in enumerate(lengths):
+        k = torch.from_numpy(get(c, "k", b, n)).cuda().to(DT[cache])
+        k[:, torch.from_numpy(r.choice(n, max(1, n // 7), replace=False)).cuda(), 3] = -math.inf
+        put(c, "k", b, k)
+    finite, nan = attend_and_check(c, q, heads, act)
+    assert finite == 4 * heads and nan == 0
+    for b, n in enumerate(lengths[1:], 1):
+        k = torch.from_numpy(get(c, "k", b, n)).cuda().to(DT[cache])
+        k[:, n // 2, 5] = math.inf                  # the queries' signs differ there
+        put(c, "k", b, k)
+    finite, nan = attend_and_check(c, q, heads, act)
+    assert finite > 0 and nan > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+def test_keys_without_a_score(act, cache, heads, kv, dim):
+    """Infinities of both signs in a key, an infinity against a zero, NaN."""
+    c = make_cache((5, 300), kv, dim, 16, cache, 15, evicts=True)
+    base = torch.randn((2, heads, dim), generator=seeded(16), device="cuda").abs() + 0.01
+    for bad in ((3, math.inf, 4, -math.inf), (6, math.inf, 6, math.inf), (1, math.nan, 1, math.nan)):
+        d = clone(c)
+        for b, n in enumerate((5, 300)):
+            k = torch.from_numpy(get(d, "k", b, n)).cuda().to(DT[cache])
+            k[0, n // 3, bad[0]], k[0, n // 3, bad[2]] = bad[1], bad[3]
+            put(d, "k", b, k)
+        q = base.clone()
+        q[:, :, 6] = 0.0
+        finite, nan = attend_and_check(d, q.reshape(2, -1).to(DT[act]), heads, act)
+        assert nan == 2 * heads // kv and finite == 2 * heads - nan
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_infinite_queries(act, cache):
+    """An infinite element of a query: tokens of the other sign are left with
+    no weight, and all scores are -inf if there are no others."""
+    c = make_cache((40, 500, 7), 2, 64, 16, cache, 25, evicts=True)
+    for b, n in enumerate((40, 500, 7)):
+        k = torch.from_numpy(get(c, "k", b, n)).cuda().to(DT[cache])
+        k[:, :, 9] = k[:, :, 9].abs() + 0.5
+        put(c, "k", b, k)
+    q = torch.randn((3, 4, 64), generator=seeded(26), device="cuda") * 1e3
+    q[0, 1, 9] = q[1, 2, 9] = -math.inf             # every score -inf: zeros
+    q[2, 3, 9] = math.inf
+    finite, nan = attend_and_check(c, q.reshape(3, 256).to(DT[act]), 4, act)
+    assert finite == 11 and nan == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", (4, 40))
+def test_keys_beyond_the_range_of_the_cache(heads):
+    """How infinities come about: float32 keys above 65504 appended to an f16 cache."""
+    c = make_cache((200, 9), 2, 64, 16, "f16", 35, room=1, evicts=True)
+    x = torch.randn((2, (heads + 4) * 64), generator=seeded(36), device="cuda")
+    x[:, 2: heads * 64: 64] = 1.0
+    x[:, heads * 64 + 2] = x[:, (heads + 1) * 64 + 2] = -1e5
+    q = torch.empty((2, heads * 64), device="cuda")
+    m.mosaic_cache_append(c, x, heads, q)
+    assert int(torch.isinf(c.k).sum()) == 4
+    finite, nan = attend_and_check(c, q, heads, "f32")
+    assert finite == 2 * heads and nan == 0
