@@ -125,6 +125,13 @@ template <> struct Matrix<MOSAIC_F32> {
   }
 };
 
+// Two 16-bit numbers of a cache, 0 in place of an infinity or NaN.
+template <int CT> __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
+  constexpr uint32_t kExponent = CT == MOSAIC_BF16 ? 0x7F80u : 0x7C00u;
+  return ((w & kExponent) == kExponent ? 0u : w & 0xFFFFu) |
+         ((w & kExponent << 16) == kExponent << 16 ? 0u : w & 0xFFFF0000u);
+}
+
 // x as the sum of PARTS 16-bit numbers, each rounded from what the ones before leave.
 template <class T, int PARTS>
 __device__ __forceinline__ void split(float x, T* part) {
@@ -460,11 +467,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
       holding = 0;
     };
 
-    // All steps of the part. Where a key or query holds an infinity, its products
-    // with the parts of the other (small ones of either sign, and zeros) can add
-    // up to NaN although the sum is infinite: `careful` takes such a score from
-    // the first parts alone, which have the signs of the whole. That is a second
-    // pass, for waves that found NaN: no step of the first has a check for it.
+    // All steps of the part. Where a key, query or value holds an infinity, its
+    // products with the parts of the other (small ones of either sign, and zeros)
+    // can add up to NaN although the sum is infinite: `careful` takes such a score
+    // from the first parts alone, which have the signs of the whole, and gives
+    // such a value to the first parts only. That is a second pass, for waves that
+    // found NaN: no step of the first has a check for it.
     auto pass = [&](auto careful) __attribute__((always_inline)) {
       constexpr bool kCareful = decltype(careful)::value;
       holding = 0;
@@ -498,7 +506,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
 #pragma unroll
               for (int s = 0; s < F::kSub; ++s) dot[s] = M::mul(key[s][c], q, dot[s]);
             }
-          if constexpr (kCareful) {
+          if constexpr (kCareful && PARTS > 1) {
             f32x4 first_part[F::kSub];
 #pragma unroll
             for (int s = 0; s < F::kSub; ++s) first_part[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -557,6 +565,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
             sum[nt] += w;
             C part[WPARTS];
             split<C, WPARTS>(w, part);
+            if constexpr (kCareful && CT == MOSAIC_F16) {
+              // a weight that no part holds is none for a finite value, but not for an infinite one
+              constexpr float kLeast = 0x1p-24f;
+              if (w > 0.0f && part[0] == (C)0.0f) {
+                part[0] = (C)kLeast;
+                part[1] = (C)-kLeast;
+              }
+            }
 #pragma unroll
             for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
           }
@@ -566,10 +582,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
         for (int v = 0; v < NV; ++v)
 #pragma unroll
           for (int j = 0; j < EV; ++j) {
-            Frag vf;
+            Frag vf, rest;                          // for the first part of the weights, and for the others
             if constexpr (F::kWide) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) vf[i] = __uint_as_float(value[i][v][j]);
+              rest = vf;
             } else {
               u32x4 w;
 #pragma unroll
@@ -577,11 +594,16 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
                 w[i] = __builtin_amdgcn_perm(value[2 * i + 1][v][j / 2], value[2 * i][v][j / 2],
                                              j % 2 ? 0x07060302u : 0x05040100u);
               vf = __builtin_bit_cast(Frag, w);
+              if constexpr (kCareful) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = finite_pair<CT>(w[i]);
+              }
+              rest = __builtin_bit_cast(Frag, w);
             }
 #pragma unroll
             for (int part = WPARTS - 1; part >= 0; --part)
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(vf, pf[nt][part], acc[nt][v][j]);
+              for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = M::mul(part > 0 ? rest : vf, pf[nt][part], acc[nt][v][j]);
           }
 #pragma unroll
         for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
@@ -590,11 +612,17 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
       if (a.accumulate) release();
     };
     pass(std::false_type());
-    if constexpr (PARTS > 1) {
-      bool nan = false;
+    if constexpr (WPARTS > 1) {
+      f32x4 most = acc[0][0][0];                    // NaN if any is
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) nan = nan || sum[nt] != sum[nt];
-      if (__any(nan)) {
+      for (int nt = 0; nt < NT; ++nt) {
+        most[0] = __builtin_elementwise_maximum(most[0], sum[nt]);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < EV; ++j) most = __builtin_elementwise_maximum(most, acc[nt][v][j]);
+      }
+      if (__any(__builtin_isunordered(most[0], most[1]) || __builtin_isunordered(most[2], most[3]))) {
 #pragma unroll
         for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
         load_keys(cur);

@@ -143,3 +143,64 @@ def test_keys_beyond_the_range_of_the_cache(heads):
     assert int(torch.isinf(c.k).sum()) == 4
     finite, nan = attend_and_check(c, q, heads, "f32")
     assert finite == 2 * heads and nan == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+def test_infinite_values(act, cache, heads, kv, dim):
+    """An infinite element of some tokens' values makes that column infinite;
+    both signs or a NaN make it NaN; no other column changes."""
+    lengths = (1, 33, 700, 3000)
+    c = make_cache(lengths, kv, dim, 16, cache, 45, evicts=True)
+    q = torch.randn((4, heads * dim), generator=seeded(46), device="cuda").to(DT[act])
+    for b, n in enumerate(lengths):
+        v = torch.from_numpy(get(c, "v", b, n)).cuda().to(DT[cache])
+        v[:, n // 2, 1], v[:, n - 1, 1] = math.inf, math.inf
+        v[:, n // 3, 4] = -math.inf
+        v[0, n // 2, 5], v[0, 0, 5] = -math.inf, math.inf
+        v[0, n // 4, 7] = math.nan
+        put(c, "v", b, v)
+    before = [get(c, "weights", b, n) for b, n in enumerate(lengths)]
+    out = torch.full_like(q, float("nan"))
+    m.mosaic_cache_attend(c, q, heads, out)
+    got = f64(out).reshape(4, kv, heads // kv, dim)
+    assert (got[..., 1] == math.inf).all() and (got[..., 4] == -math.inf).all()
+    assert np.isnan(got[1:, 0, :, 5]).all() and np.isnan(got[:, 0, :, 7]).all()
+    assert np.isfinite(np.delete(got, [1, 4, 5, 7], axis=-1)).all()
+    attend_and_check(c, q, heads, act)
+    # the rest to the same bits as without them
+    d = clone(c)
+    for b, n in enumerate(lengths):
+        put(d, "v", b, torch.nan_to_num(torch.from_numpy(get(c, "v", b, n)).cuda(), 0.0, 0.0, 0.0).to(DT[cache]))
+        put(d, "weights", b, torch.from_numpy(before[b]).cuda().float())
+    plain = torch.full_like(q, float("nan"))
+    m.mosaic_cache_attend(d, q, heads, plain, accumulate=True)
+    assert np.array_equal(np.delete(got, [1, 4, 5, 7], axis=-1),
+                          np.delete(f64(plain).reshape(got.shape), [1, 4, 5, 7], axis=-1))
+    for b, n in enumerate(lengths):
+        assert np.array_equal(get(c, "weights", b, n), get(d, "weights", b, n))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,cache", TYPES)
+def test_infinite_values_of_little_weight(act, cache):
+    """A weight of e^-40 is none for finite values and makes infinite ones
+    infinite; a weight of none (a score of -inf) makes them NaN."""
+    c = make_cache((300, 20), 1, 64, 16, cache, 55, evicts=True)
+    for b, n in enumerate((300, 20)):
+        k = torch.from_numpy(get(c, "k", b, n)).cuda().to(DT[cache])
+        v = torch.from_numpy(get(c, "v", b, n)).cuda().to(DT[cache])
+        k[:, :, 0] = 0.0
+        k[:, 7, 0], v[:, 7, 2] = -40.0, math.inf
+        k[:, 9, 0], v[:, 9, 3] = -40.0, 3.0
+        k[:, 11, 0], v[:, 11, 4] = -math.inf, -math.inf
+        put(c, "k", b, k), put(c, "v", b, v)
+    q = torch.zeros((2, 2, 64), device="cuda")
+    q[:, :, 0] = 8.0                                # scores are the keys' first elements
+    attend_and_check(c, q.reshape(2, 128).to(DT[act]), 2, act)
+    out = torch.empty((2, 128), dtype=DT[act], device="cuda")
+    m.mosaic_cache_attend(c, q.reshape(2, 128).to(DT[act]), 2, out)
+    got = f64(out).reshape(2, 2, 64)
+    assert (got[..., 2] == math.inf).all() and np.isnan(got[..., 4]).all()
+    assert np.isfinite(np.delete(got, [2, 4], axis=-1)).all()
