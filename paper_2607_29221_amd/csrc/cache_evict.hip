@@ -507,7 +507,9 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
 // Copies rows along the pairs of slots, 16 bytes per thread. Bound by the rows'
 // traffic: 63 MB in and out in 14.7 us for the 131072 -> 8192 case, in 16.4 us
 // with 64 moves per workgroup (more rounds of dependent loads for a thread).
-constexpr int32_t kMovesPerBlock = 16;
+// A launch takes less than 2^32 threads along an axis, so beyond kMostBlocks
+// workgroups they go on to further moves.
+constexpr int32_t kMovesPerBlock = 16, kMostBlocks = 1 << 16;
 __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t moves) {
   const int h = blockIdx.y, b = blockIdx.z;
   const int64_t bh = (int64_t)b * a.c.kv_heads + h;
@@ -519,22 +521,24 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
   }
   if (moves == 0) return;
   const Lists l = lists_of(a, moves, bh);
-  const int32_t all = *l.count, first = (int32_t)blockIdx.x * kMovesPerBlock;
-  const int32_t count = min(all - first, kMovesPerBlock);
+  const int32_t all = *l.count;
   const int32_t chunks = a.c.head_dim * (a.c.dtype == MOSAIC_F32 ? 4 : 2) / 16;
-  for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {
-    const int32_t m = w / chunks, c = w - m * chunks;
-    const int32_t from = l.movers[all - 1 - (first + m)], to = l.free_slots[first + m];
-    const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);   // both are there: see rank_key
-    const int64_t of = row_offset(a.c, pf, h, from) + 16 * c, ot = row_offset(a.c, pt, h, to) + 16 * c;
-    const u32x4 k = *(const u32x4*)(a.c.k + of), v = *(const u32x4*)(a.c.v + of);
-    *(u32x4*)(a.c.k + ot) = k;
-    *(u32x4*)(a.c.v + ot) = v;
-    if (c == 0) {
-      const int64_t rf = row_index(a.c, pf, h, from), rt = row_index(a.c, pt, h, to);
-      a.new_weights[rt] = a.c.weights[rf];
-      a.new_order[rt] = a.c.order[rf];
-      if (a.kept != nullptr) a.kept[bh * a.budget + to] = from;
+  for (int32_t first = (int32_t)blockIdx.x * kMovesPerBlock; first < all; first += (int32_t)gridDim.x * kMovesPerBlock) {
+    const int32_t count = min(all - first, kMovesPerBlock);
+    for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {
+      const int32_t m = w / chunks, c = w - m * chunks;
+      const int32_t from = l.movers[all - 1 - (first + m)], to = l.free_slots[first + m];
+      const int32_t pf = page_of(a.c, b, from), pt = page_of(a.c, b, to);   // both are there: see rank_key
+      const int64_t of = row_offset(a.c, pf, h, from) + 16 * c, ot = row_offset(a.c, pt, h, to) + 16 * c;
+      const u32x4 k = *(const u32x4*)(a.c.k + of), v = *(const u32x4*)(a.c.v + of);
+      *(u32x4*)(a.c.k + ot) = k;
+      *(u32x4*)(a.c.v + ot) = v;
+      if (c == 0) {
+        const int64_t rf = row_index(a.c, pf, h, from), rt = row_index(a.c, pt, h, to);
+        a.new_weights[rt] = a.c.weights[rf];
+        a.new_order[rt] = a.c.order[rf];
+        if (a.kept != nullptr) a.kept[bh * a.budget + to] = from;
+      }
     }
   }
 }
@@ -565,8 +569,8 @@ hipError_t launch_cache_evict(const EvictLaunch& a, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned blocks = moves > 0 ? (unsigned)((moves + kMovesPerBlock - 1) / kMovesPerBlock) : 1u;
-  cache_move_kernel<<<dim3(blocks, a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, moves);
+  const int64_t blocks = moves > 0 ? (moves + kMovesPerBlock - 1) / kMovesPerBlock : 1;
+  cache_move_kernel<<<dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), a.c.kv_heads, a.c.batch), 256, 0, s>>>(a, moves);
   return hipGetLastError();
 }
 
