@@ -53,7 +53,8 @@ class CachedDecoder:
 
     ``dtype`` is the cache's (activations are float32). ``table`` and
     ``sections`` give rotary positions (mosaic.Rotary; None: none, as in
-    decoder.py). ``budget``: tokens that a head keeps after every call, the
+    decoder.py); calls without ``positions`` turn a token by its number, up to
+    the table's last row. ``budget``: tokens that a head keeps after every call, the
     ``recent`` latest among them; None keeps all."""
 
     def __init__(self, linear: Linear, layers: int, cfg: dict, max_len: int, dtype=torch.float32, page_size: int = 64,
@@ -68,7 +69,12 @@ class CachedDecoder:
         self.caches: List[m.KVCache] = [
             m.KVCache.empty(cfg["batch"], max_len, cfg["kv_heads"], cfg["head_dim"], dtype, page_size,
                             evicts=budget is not None, device=device) for _ in range(layers)]
-        self.held = 0                        # tokens per sequence, the same in every layer
+        self.held = self.seen = 0            # tokens per sequence, the same in every layer; evicted ones among the seen
+
+    def _check_places(self, tokens: int, positions) -> None:
+        if self.table is not None and positions is None and self.seen + tokens > self.table.shape[0]:
+            raise ValueError(f"the rotary table has {self.table.shape[0]} places, {self.seen} tokens were seen before "
+                             f"these {tokens}")
 
     def _append(self, cache: m.KVCache, qkv: torch.Tensor, starts, positions) -> torch.Tensor:
         cfg = self.cfg
@@ -98,8 +104,9 @@ class CachedDecoder:
             raise ValueError("a prompt needs an empty cache, and sequences of one length")
         if n > self.caches[0].slots:
             raise ValueError(f"a prompt of {n} tokens does not fit {self.caches[0].slots} slots")
+        self._check_places(n, positions)
         starts = torch.arange(B + 1, dtype=torch.int32, device=x.device) * n
-        self.held = n
+        self.held = self.seen = n
 
         def attend(cache: m.KVCache, qkv: torch.Tensor) -> torch.Tensor:
             q = self._append(cache, qkv, starts, positions)
@@ -123,7 +130,9 @@ class CachedDecoder:
             raise ValueError("a step takes one token per sequence")
         if self.held >= self.caches[0].slots:
             raise ValueError(f"no slot is free: {self.held} tokens are held")
+        self._check_places(1, positions)
         self.held += 1
+        self.seen += 1
 
         def attend(cache: m.KVCache, qkv: torch.Tensor) -> torch.Tensor:
             q = self._append(cache, qkv, None, positions)

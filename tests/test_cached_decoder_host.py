@@ -1,0 +1,76 @@
+"""What CachedDecoder keeps count of and refuses, without a GPU: the operators
+are replaced by ones that advance the caches' state."""
+import pytest
+import torch
+
+from paper_2607_29221_amd import mosaic as m
+from paper_2607_29221_amd.cached_decoder import CachedDecoder
+
+CFG = dict(hidden=8, heads=2, kv_heads=1, head_dim=8, ffn=4, layers=2, batch=2, seq=5)
+WIDTH = {"qkv": 32, "o": 8, "gate_up": 8, "down": 8}
+
+
+@pytest.fixture(autouse=True)
+def operators(monkeypatch):
+    def append(cache, qkv, heads, q_out, starts=None, rotary=None, new_state=None):
+        q_out.zero_()
+        cache.state += qkv.shape[0] // cache.batch
+
+    def attend(cache, q, heads, out, max_len=None, scale=None, accumulate=False):
+        assert max_len == int(cache.state[0].max())
+        out.zero_()
+
+    def evict(cache, budget, recent, max_len=None, **kw):
+        assert max_len == int(cache.state[0].max())
+        cache.state[0].clamp_(max=budget)
+    for name, f in (("append", append), ("attend", attend), ("evict", evict)):
+        monkeypatch.setattr(m, "mosaic_cache_" + name, f)
+
+
+def linear(layer, name, x):
+    return torch.zeros(x.shape[0], WIDTH[name])
+
+
+def decoder(max_len=64, lin=linear, **kw):
+    return CachedDecoder(lin, 2, CFG, max_len, page_size=16, device="cpu", **kw)
+
+
+def rows(n):
+    return torch.zeros(2 * n, 8)
+
+
+@pytest.mark.parametrize("budget", (None, 4))
+def test_numbers_beyond_the_rotary_table(budget):
+    """With a budget the tokens held stay few while their numbers go on."""
+    table = m.Rotary.frequencies(10, 4, device="cpu")
+    d = decoder(table=table, sections=[4], budget=budget)
+    with pytest.raises(ValueError, match="rotary table"):
+        d.prompt(rows(11))
+    d.prompt(rows(7))
+    for _ in range(3):
+        d.step(rows(1))
+    assert d.seen == 10 and d.held == (10 if budget is None else 4)
+    with pytest.raises(ValueError, match="rotary table"):
+        d.step(rows(1))
+    assert d.seen == 10
+    d.step(rows(1), positions=torch.tensor([[3, 9]], dtype=torch.int32))      # places of the caller's
+    with pytest.raises(ValueError, match="rotary table"):
+        d.step(rows(1))
+    free = decoder(budget=budget)                                              # nothing is turned
+    free.prompt(rows(30))
+    free.step(rows(1))
+
+
+@pytest.mark.gpu
+def test_on_the_device(monkeypatch):
+    """The device's count is the decoder's."""
+    monkeypatch.undo()
+    table = m.Rotary.frequencies(10, 4)
+    d = CachedDecoder(lambda layer, name, x: torch.zeros(x.shape[0], WIDTH[name], device="cuda"), 2, CFG, 64,
+                      page_size=16, budget=4, table=table, sections=[4])
+    d.prompt(rows(7).cuda())
+    for _ in range(3):
+        d.step(rows(1).cuda())
+    assert all(c.state.tolist() == [[4, 4], [10, 10]] for c in d.caches) and d.seen == 10
+    with pytest.raises(ValueError, match="rotary table"):
+        d.step(rows(1).cuda())
