@@ -60,6 +60,8 @@ class CachedDecoder:
     def __init__(self, linear: Linear, layers: int, cfg: dict, max_len: int, dtype=torch.float32, page_size: int = 64,
                  budget: Optional[int] = None, recent: int = 0, table: Optional[torch.Tensor] = None,
                  sections: Optional[Sequence[int]] = None, interleaved: bool = False, device="cuda"):
+        if budget is not None and budget < 1:
+            raise ValueError("a budget keeps at least one token")
         if budget is not None and not 0 <= recent <= budget:
             raise ValueError("recent must lie between 0 and the budget")
         if (table is None) != (sections is None):

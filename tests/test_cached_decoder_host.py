@@ -74,3 +74,10 @@ def test_on_the_device(monkeypatch):
     assert all(c.state.tolist() == [[4, 4], [10, 10]] for c in d.caches) and d.seen == 10
     with pytest.raises(ValueError, match="rotary table"):
         d.step(rows(1).cuda())
+
+
+@pytest.mark.parametrize("budget", (0, -1))
+def test_a_budget_of_nothing(budget):
+    """Refused at once, not in the first layer that evicts."""
+    with pytest.raises(ValueError, match="budget"):
+        decoder(budget=budget)
