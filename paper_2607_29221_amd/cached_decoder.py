@@ -55,7 +55,9 @@ class CachedDecoder:
     ``sections`` give rotary positions (mosaic.Rotary; None: none, as in
     decoder.py); calls without ``positions`` turn a token by its number, up to
     the table's last row. ``budget``: tokens that a head keeps after every call, the
-    ``recent`` latest among them; None keeps all."""
+    ``recent`` latest among them; None keeps all. Where the slots are as many
+    as the budget the caches get room for the token that comes on top; a
+    larger budget is never reached, and a full cache ends the decode."""
 
     def __init__(self, linear: Linear, layers: int, cfg: dict, max_len: int, dtype=torch.float32, page_size: int = 64,
                  budget: Optional[int] = None, recent: int = 0, table: Optional[torch.Tensor] = None,
@@ -66,6 +68,8 @@ class CachedDecoder:
             raise ValueError("recent must lie between 0 and the budget")
         if (table is None) != (sections is None):
             raise ValueError("rotary positions need a table and sections")
+        if budget is not None and budget == -(-max_len // page_size) * page_size:
+            max_len = budget + 1             # the next token comes before the one that it replaces goes
         self.linear, self.cfg, self.budget, self.recent = linear, cfg, budget, recent
         self.table, self.sections, self.interleaved = table, sections, interleaved
         self.caches: List[m.KVCache] = [

@@ -81,3 +81,21 @@ def test_a_budget_of_nothing(budget):
     """Refused at once, not in the first layer that evicts."""
     with pytest.raises(ValueError, match="budget"):
         decoder(budget=budget)
+
+
+@pytest.mark.parametrize("max_len", (32, 30, 48))
+def test_as_many_slots_as_the_budget(max_len):
+    """A decode at its budget goes on without end; max_len 30 makes 32 slots."""
+    d = decoder(max_len, budget=32)
+    d.prompt(rows(31))
+    for _ in range(10):
+        d.step(rows(1))
+    assert d.held == 32 and d.seen == 41
+
+
+def test_a_budget_beyond_the_slots():
+    d = decoder(32, budget=33)
+    d.prompt(rows(31))
+    d.step(rows(1))
+    with pytest.raises(ValueError, match="no slot"):
+        d.step(rows(1))
