@@ -57,7 +57,12 @@ class CachedDecoder:
     the table's last row. ``budget``: tokens that a head keeps after every call, the
     ``recent`` latest among them; None keeps all. Where the slots are as many
     as the budget the caches get room for the token that comes on top; a
-    larger budget is never reached, and a full cache ends the decode."""
+    larger budget is never reached, and a full cache ends the decode.
+
+    A call that raises (a linear layer of a server that cannot be reached, or
+    whose products fail their check) leaves the decoder as it was, and can be
+    made again; with a budget, a step that fails after its first layer's q|k|v
+    product cannot be undone, and further calls are refused."""
 
     def __init__(self, linear: Linear, layers: int, cfg: dict, max_len: int, dtype=torch.float32, page_size: int = 64,
                  budget: Optional[int] = None, recent: int = 0, table: Optional[torch.Tensor] = None,
@@ -76,6 +81,7 @@ class CachedDecoder:
             m.KVCache.empty(cfg["batch"], max_len, cfg["kv_heads"], cfg["head_dim"], dtype, page_size,
                             evicts=budget is not None, device=device) for _ in range(layers)]
         self.held = self.seen = 0            # tokens per sequence, the same in every layer; evicted ones among the seen
+        self.torn = False                    # a call failed and left tokens in some layers only
 
     def _check_places(self, tokens: int, positions) -> None:
         if self.table is not None and positions is None and self.seen + tokens > self.table.shape[0]:
@@ -89,21 +95,47 @@ class CachedDecoder:
         m.mosaic_cache_append(cache, qkv, cfg["heads"], q, starts=starts, rotary=rotary)
         return q
 
-    def _layers(self, h: torch.Tensor, attend) -> torch.Tensor:
-        F = self.cfg["ffn"]
-        for i, cache in enumerate(self.caches):
-            h = h + self.linear(i, "o", attend(cache, self.linear(i, "qkv", rms_norm(h).contiguous())))
-            gu = self.linear(i, "gate_up", rms_norm(h).contiguous())
-            h = h + self.linear(i, "down", (torch.nn.functional.silu(gu[:, :F]) * gu[:, F:]).contiguous())
-            if self.budget is not None and self.held > self.budget:
-                m.mosaic_cache_evict(cache, self.budget, self.recent, max_len=self.held)
-        if self.budget is not None:
-            self.held = min(self.held, self.budget)
+    def _layers(self, h: torch.Tensor, tokens: int, attend) -> torch.Tensor:
+        """All layers over ``tokens`` new tokens of each sequence;
+        attend(cache, qkv, held) appends them, which makes ``held`` in all. The
+        counts advance once the last layer is through."""
+        F, held, started = self.cfg["ffn"], self.held + tokens, False
+        try:
+            for i, cache in enumerate(self.caches):
+                qkv = self.linear(i, "qkv", rms_norm(h).contiguous())
+                started = True
+                h = h + self.linear(i, "o", attend(cache, qkv, held))
+                gu = self.linear(i, "gate_up", rms_norm(h).contiguous())
+                h = h + self.linear(i, "down", (torch.nn.functional.silu(gu[:, :F]) * gu[:, F:]).contiguous())
+                if self.budget is not None and held > self.budget:
+                    m.mosaic_cache_evict(cache, self.budget, self.recent, max_len=held)
+        except BaseException:
+            if started:
+                self._take_back()
+            raise
+        self.held = held if self.budget is None else min(held, self.budget)
+        self.seen += tokens
         return h
+
+    def _take_back(self) -> None:
+        """The caches as before a call that failed in the middle of the layers.
+        What lies behind the tokens held has no meaning; the weights that the
+        call added to theirs, and what it evicted, cannot be undone."""
+        self.torn = self.budget is not None and self.held > 0
+        if not self.torn:
+            for cache in self.caches:
+                cache.state[0].fill_(self.held)
+                cache.state[1].fill_(self.seen)
+
+    def _check_whole(self) -> None:
+        if self.torn:
+            raise RuntimeError("an earlier step failed in the middle of the layers, after it had changed weights and "
+                               "tokens of some: this decoder's caches cannot be used any more")
 
     def prompt(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Hidden states (batch * seq x hidden) of a prompt, sequence after
         sequence, into an empty cache; ``positions``: axes x rows."""
+        self._check_whole()
         B = self.cfg["batch"]
         n = x.shape[0] // B
         if self.held != 0 or n * B != x.shape[0]:
@@ -112,9 +144,8 @@ class CachedDecoder:
             raise ValueError(f"a prompt of {n} tokens does not fit {self.caches[0].slots} slots")
         self._check_places(n, positions)
         starts = torch.arange(B + 1, dtype=torch.int32, device=x.device) * n
-        self.held = self.seen = n
 
-        def attend(cache: m.KVCache, qkv: torch.Tensor) -> torch.Tensor:
+        def attend(cache: m.KVCache, qkv: torch.Tensor, held: int) -> torch.Tensor:
             q = self._append(cache, qkv, starts, positions)
             heads, dim, page = self.cfg["heads"], self.cfg["head_dim"], cache.k.shape[2]
             out = torch.empty_like(q)
@@ -127,24 +158,23 @@ class CachedDecoder:
                     cache.weights[where, :, off] += got.t()
             return out
 
-        return self._layers(x, attend)
+        return self._layers(x, n, attend)
 
     def step(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Hidden states of the next token (batch x hidden; positions: axes x
         batch), one per sequence."""
+        self._check_whole()
         if x.shape[0] != self.cfg["batch"]:
             raise ValueError("a step takes one token per sequence")
         if self.held >= self.caches[0].slots:
             raise ValueError(f"no slot is free: {self.held} tokens are held")
         self._check_places(1, positions)
-        self.held += 1
-        self.seen += 1
 
-        def attend(cache: m.KVCache, qkv: torch.Tensor) -> torch.Tensor:
+        def attend(cache: m.KVCache, qkv: torch.Tensor, held: int) -> torch.Tensor:
             q = self._append(cache, qkv, None, positions)
             out = torch.empty_like(q)
-            m.mosaic_cache_attend(cache, q, self.cfg["heads"], out, max_len=self.held,
+            m.mosaic_cache_attend(cache, q, self.cfg["heads"], out, max_len=held,
                                   accumulate=cache.weights is not None)
             return out
 
-        return self._layers(x, attend)
+        return self._layers(x, 1, attend)

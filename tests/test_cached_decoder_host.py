@@ -99,3 +99,85 @@ def test_a_budget_beyond_the_slots():
     d.step(rows(1))
     with pytest.raises(ValueError, match="no slot"):
         d.step(rows(1))
+
+
+class _Fails:
+    """Linear layers of which one raises once."""
+
+    def __init__(self, layer, name):
+        self.at = (layer, name)
+
+    def __call__(self, layer, name, x):
+        if (layer, name) == self.at:
+            self.at = None
+            raise ConnectionError("no answer")
+        return linear(layer, name, x)
+
+
+WHERE = [(layer, name) for layer in range(2) for name in WIDTH]
+
+
+def states(d):
+    return [c.state.tolist() for c in d.caches]
+
+
+@pytest.mark.parametrize("layer,name", WHERE)
+@pytest.mark.parametrize("budget", (None, 4, 40))
+def test_a_prompt_that_fails_can_be_made_again(layer, name, budget):
+    d = decoder(lin=_Fails(layer, name), budget=budget)
+    with pytest.raises(ConnectionError):
+        d.prompt(rows(7))
+    assert d.held == d.seen == 0 and states(d) == [[[0, 0], [0, 0]]] * 2
+    d.prompt(rows(6))
+    n = 6 if budget != 4 else 4
+    assert d.held == n and d.seen == 6 and states(d) == [[[n, n], [6, 6]]] * 2
+
+
+@pytest.mark.parametrize("layer,name", WHERE)
+@pytest.mark.parametrize("budget", (None, 4, 40))
+def test_a_step_that_fails(layer, name, budget):
+    d = decoder(budget=budget)
+    d.prompt(rows(7))
+    before = states(d)
+    d.linear = _Fails(layer, name)
+    with pytest.raises(ConnectionError):
+        d.step(rows(1))
+    if budget is not None and (layer, name) != (0, "qkv"):
+        for call in (d.step, d.prompt):
+            with pytest.raises(RuntimeError, match="cannot be used"):
+                call(rows(1))
+        return
+    assert d.seen == 7 and states(d) == before
+    d.step(rows(1))
+    n = 8 if budget != 4 else 4
+    assert d.held == n and d.seen == 8 and states(d) == [[[n, n], [8, 8]]] * 2
+
+
+@pytest.mark.gpu
+def test_a_failed_step_on_the_device(monkeypatch):
+    """The same hidden states with a failure in between as without."""
+    monkeypatch.undo()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w = {n: torch.randn((o, 4 if n == "down" else 8), generator=g, device="cuda") for n, o in
+         (("qkv", 32), ("o", 8), ("gate_up", 8), ("down", 8))}
+    w["o"] = torch.randn((8, 16), generator=g, device="cuda")
+    x = torch.randn((2 * 9, 8), generator=g, device="cuda")
+    table = m.Rotary.frequencies(10, 4)
+
+    def lin(layer, name, a):
+        return a @ w[name].t()
+
+    def run(fail):
+        d = CachedDecoder(lin, 2, CFG, 64, page_size=16, table=table, sections=[4])
+        outs = []
+        for part in (x[:14], x[14:16], x[16:]):
+            call = d.prompt if part.shape[0] > 2 else d.step
+            if fail:
+                failing = _Fails(1, "gate_up")
+                d.linear = lambda l, n, a: failing(l, n, a) if (l, n) == failing.at else lin(l, n, a)
+                with pytest.raises(ConnectionError):
+                    call(part + 1.0)
+                d.linear = lin
+            outs.append(call(part))
+        return torch.cat(outs)
+    assert torch.equal(run(False), run(True))
