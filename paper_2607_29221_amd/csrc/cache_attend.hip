@@ -19,9 +19,11 @@
 //   of 8 tokens' rows and turns them with byte permutes (32 for 32 tokens of
 //   128), so nothing passes through LDS.
 // * Over a 16-bit cache, float32 queries and all weights are split into 16-bit
-//   parts (float32 activations: three of bf16, two of f16 with the range
-//   centred; 16-bit ones: two for the weights) that are multiplied one after
-//   the other into the same sums, so nothing but the stored types is rounded.
+//   parts that are multiplied one after the other into the same sums. Three of
+//   bf16 (float32 activations) hold all 24 bits. Two of f16, the range centred,
+//   leave out at most 2^-23 of a number, less than the sums' own rounding, and two
+//   of bf16 (16-bit activations) at most 2^-17 of a weight: a five hundredth
+//   of what rounding the output to bf16 leaves out of it.
 //   The matrix cores have room for it (a sixth of their rate at full
 //   bandwidth): 64 sequences take 162 us with bf16 and with float32.
 // * M is raised, and O rescaled, only when a score passes it by more than
@@ -89,7 +91,7 @@ template <int CT, int XT, int DP> struct Form {
   typedef typename FloatType<XT>::type X;
   static constexpr bool kWide = CT == MOSAIC_F32;
   // 16-bit numbers that make up a query's element (one if it is one) and a
-  // weight (16-bit activations: enough that only the output's rounding shows)
+  // weight (16-bit activations: enough that the output's rounding is the larger)
   static constexpr int kParts = kWide || XT != MOSAIC_F32 ? 1 : CT == MOSAIC_BF16 ? 3 : 2;
   static constexpr int kWeightParts = kWide ? 1 : XT != MOSAIC_F32 || CT == MOSAIC_F16 ? 2 : 3;
   static constexpr int kSub = kWide ? 1 : 2;                // blocks of 16 tokens
