@@ -127,12 +127,16 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
  *     out_g = sum_i p_i v_i,
  * zeros for a sequence without tokens. Infinities and NaN among the tokens act
  * as in these formulas (a score of -inf is no weight; zeros if there is no
- * other). Scores, softmax sums and outputs are accumulated in float32. ``accumulate`` nonzero adds p_i of every head of
- * the group to ``weights`` of slot i and head h (without atomics: two runs
- * give the same bits). q and out are batch x heads * head_dim of x_dtype
- * (MOSAIC_F32 or the cache's type), 16-byte aligned, ldq and ldo multiples of
- * 16 bytes, not overlapping. lengths: batch entries, e.g. the first row of
- * the state. */
+ * other). Scores, softmax sums and outputs are accumulated in float32, outputs
+ * before the division and with weights of up to 2^8: a value above 2^119 over
+ * the number of tokens may overflow there. ``accumulate`` nonzero adds p_i of
+ * every head of the group to ``weights`` of slot i and head h (without atomics:
+ * two runs give the same bits). q and out are batch x heads * head_dim of
+ * x_dtype (MOSAIC_F32 or the cache's type), 16-byte aligned, ldq and ldo
+ * multiples of 16 bytes, not overlapping. lengths: batch entries, e.g. the
+ * first row of the state. The workspace of a call that accumulates holds every
+ * score, batch x heads x max_len floats: there max_len should be no larger than
+ * it has to be. */
 mosaic_status mosaic_cache_attend_workspace(const mosaic_kv_cache* cache, int32_t heads, int64_t max_len,
                                             int32_t accumulate, int64_t* bytes);
 mosaic_status mosaic_cache_attend(const mosaic_kv_cache* cache, const void* q, int64_t ldq, int32_t x_dtype,

@@ -7,7 +7,7 @@
 // cosines and sines into LDS once and every head reads them from there, so a
 // row of q|k|v is read once and every output written once, and the call is
 // bound by that traffic: 4096 tokens of 64 + 2 * 8 heads of 128 floats in 61 us
-// (5.5 TB/s). A single token takes 3.2 us and 48 take 3.7 us, the latency of
+// (5.5 TB/s). A single token takes 3.3 us and 48 take 3.7 us, the latency of
 // launch, state, page and table; its row is asked for before these.
 #include "cache.h"
 #include "device_common.h"
@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kFewRows = 256;     // no more than one workgroup per compute unit
 // Rows that the 32 MiB of second-level cache cannot hold pass by it (168 MB of
-// q|k|v: 61 us, 68 us through it); fewer are left there for the attention that
+// q|k|v: 61 us, 69 us through it); fewer are left there for the attention that
 // comes next.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 

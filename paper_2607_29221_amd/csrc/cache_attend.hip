@@ -24,8 +24,8 @@
 //   leave out at most 2^-23 of a number, less than the sums' own rounding, and two
 //   of bf16 (16-bit activations) at most 2^-17 of a weight: a five hundredth
 //   of what rounding the output to bf16 leaves out of it.
-//   The matrix cores have room for it (a sixth of their rate at full
-//   bandwidth): 64 sequences take 162 us with bf16 and with float32.
+//   The matrix cores have room for it (busy 14% of the time at full bandwidth
+//   with three parts): 64 sequences take 165 us with bf16, 164 us with float32.
 // * M is raised, and O rescaled, only when a score passes it by more than
 //   kSlack: sums of up to 2^kSlack are as exact as sums of up to 1.
 // * All tokens of a key/value head, one sequence after the other, are cut into
@@ -152,8 +152,8 @@ __device__ __forceinline__ void split(float x, T* part) {
 constexpr int kStepTokens = 128;
 // Workgroups go to the chip's dies in turn. The blocks of query heads of a
 // share lie this far apart, so that they read its keys and values through one
-// die's L2 (64 query heads on one key/value head: 83 us side by side, 75 us so,
-// and 71 us with the shares that fit).
+// die's L2 (64 query heads on one key/value head, 64 sequences of up to 16000
+// tokens, this kernel alone: 91 us side by side, 75 us so).
 constexpr int kXcds = 8;
 
 // The workspace: per slot and query head the base and the sum of the weights
@@ -179,15 +179,15 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // A workgroup per compute unit, or as many as there are steps: its four
   // waves keep 64 KiB of a bf16 cache's rows of 128 in flight, which is
   // enough, and every further workgroup is another part to join (64 sequences
-  // with the join: 162 us with 256 workgroups in all, 165 us with 512, 169 us
-  // with 768; heads of 256 elements 89, 92 and 101 us). Where several blocks of
-  // query heads read the same keys, arithmetic counts too and two per unit hide
-  // each other's waits (128 heads on one key/value head, bf16 cache: 173 us
-  // with one, 130 to 142 us with two; heads of 256 elements, where the registers hold
-  // one, 79 and 85 us). Never more than fit at once, since a unit with two
-  // takes twice as long (12 key/value heads: 256 us with 264, 174 us with 252),
-  // but more per unit where more than one unit in 16 would idle (71 heads: 289
-  // us with 213, 250 us with 497).
+  // with the join: 164 us with 256 workgroups in all, 166 us with 512, 168 us
+  // with 768; 8 heads of 256 elements on one 52, 59 and 66 us). Where several
+  // blocks of query heads read the same keys, two per unit hide each other's
+  // waits (128 heads on one key/value head, kernel alone: float32 over bf16 178
+  // us with one, 142 us with two; bf16 122 and 117 us; 48 heads of 256 elements,
+  // where the registers hold one, 178 and 180 us). Never more than fit at
+  // once, since a unit with two takes twice as long (12 key/value heads: 249 us
+  // with 264, 173 us with 252), but more per unit where more than one unit in 16
+  // would idle (71 heads: 217 us with 213, 186 us with 497).
   int32_t slots = p.tile_groups > 1 && c.head_dim <= 128 ? 512 : 256;
   int64_t wanted;
   while (true) {
@@ -262,21 +262,21 @@ __device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int 
 constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : (DP == 128 ? 3 : 4) - (NT - 1); }
 
 // NT: blocks of 16 query heads per wave (64 query heads on one key/value head
-// of 128 elements, 64 sequences: 105 us with one, 71 us with two; four
-// leave the registers one wave per SIMD and took up to a fifth longer with
-// float32 activations).
+// of 128 elements, 64 sequences: 111 us with one, 75 us with two; four would
+// leave the registers one wave per SIMD).
 // STREAM: no other workgroup reads the same keys and values, so they pass by
-// the caches (131072 tokens: 92 us through them, 81 us past them); where
-// several do (groups of more than 32 heads) they go through (the 64 heads: 71
-// us, 83 us past).
+// the caches (131072 tokens: 92 us through them, 80 us past them); where
+// several do (groups of more than 32 heads) they go through (the 64 heads: 75
+// us, 88 us past).
 // Measured on an MI355X, this kernel alone, heads of 128 elements, 64 query
-// and 8 key/value heads: 131072 tokens of one sequence 81 us (6.6 TB/s of keys
-// and values); 64 sequences of 512 to 7168 tokens 157 us (6.6 TB/s); 32 heads
-// of each, float32 cache, 120 us (6.2 TB/s); 1024 tokens 7 us, the latency of
-// its chain of loads. With weights the 64 sequences take 216 us: the 63 MB of
-// scores cost more than their share of the traffic (205 us with half of them
-// stored), whether one step's or many steps' are stored at a time, past the
-// caches or through them.
+// and 8 key/value heads: 131072 tokens of one sequence 80 us (6.7 TB/s of keys
+// and values); 64 sequences of 512 to 7168 tokens 161 us (6.4 TB/s); 32 heads
+// of each, float32 cache, 122 us (6.2 TB/s); 1024 tokens 7 us, the latency of
+// its chain of loads. With weights the 64 sequences take 217 us: storing 63 MB
+// of scores costs several times their share of the traffic, whether one
+// step's or many steps' are stored at a time, past the caches or through them.
+// Loads that wait behind a wave's stores, with one wave per SIMD and nothing
+// to cover the wait, would explain it; that is not shown.
 template <int CT, int XT, int DP, int NT, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef Form<CT, XT, DP> F;

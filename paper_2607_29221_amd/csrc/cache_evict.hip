@@ -15,12 +15,11 @@
 // finds the digit before it from the counts of all chunks), then the numbering.
 //
 // Measured on an MI355X, 8 key/value heads: 64 sequences of 2049 tokens to
-// 2048: 8.7 us for the selection (21 MB of weights, order and slots in and
-// out: 2.4 TB/s, half of it latency) and 3 us for one row per head; four of up
-// to 7168 to 1024: 11.4 us, the latency of its steps on 32 workgroups, and
-// 11.7 us for 50 MB of float32 rows; one of 131072 to 8192: 7 + 6.4 + 6.8 + 9
-// us in place of 353 us for one workgroup per head with its keys in memory,
-// and 15 us for 62 MB of rows.
+// 2048: 8.9 us for the selection (21 MB of weights, order and slots in and
+// out: 2.4 TB/s, half of it latency) and 3.4 us for one row per head; four of up
+// to 7168 to 1024: 12 us, the latency of its steps on 32 workgroups, and
+// 11.6 us for 50 MB of float32 rows; one of 131072 to 8192: 7.6 + 6.3 + 6.8 +
+// 8.8 us, and 15.3 us for 62 MB of rows.
 #include "cache.h"
 #include "device_common.h"
 #include "dispatch.h"
@@ -32,7 +31,7 @@ constexpr int kBins = 2048;
 constexpr int kShortSlots = 8192;
 constexpr int kChunk = 8192, kChunkThreads = 1024, kChunkKeys = kChunk / kChunkThreads;
 // Evictions that are found one by one: a loop at its budget has one per step
-// (2049 to 2048 with 256 threads per head: 10 us, 26 us by digits).
+// (64 sequences of 2049 to 2048: 8.9 us, 13.8 us by digits).
 constexpr int kFew = 4;
 
 // Rank of a slot; a larger key stays before a smaller one. The latest tokens
@@ -505,7 +504,7 @@ __global__ __launch_bounds__(kChunkThreads) void cache_number_kernel(EvictLaunch
 }
 
 // Copies rows along the pairs of slots, 16 bytes per thread. Bound by the rows'
-// traffic: 63 MB in and out in 14.7 us for the 131072 -> 8192 case, in 16.4 us
+// traffic: 63 MB in and out in 15.4 us for the 131072 -> 8192 case, in 15.7 us
 // with 64 moves per workgroup (more rounds of dependent loads for a thread).
 // A launch takes less than 2^32 threads along an axis, so beyond kMostBlocks
 // workgroups they go on to further moves.

@@ -691,7 +691,9 @@ def mosaic_cache_attend(cache: KVCache, q: torch.Tensor, heads: int, out: torch.
     """out[b] = attention of q[b] (one new token, ``heads`` heads) over the
     tokens that sequence b holds; ``accumulate`` adds the attention weights
     up in cache.weights. ``max_len``: no sequence holds more tokens (None: as
-    many as there are slots). ``scale`` defaults to 1 / sqrt(head_dim)."""
+    many as there are slots); with ``accumulate`` the call takes batch x heads
+    x max_len floats of memory for its scores. ``scale`` defaults to 1 /
+    sqrt(head_dim)."""
     st = (_b or _native()).cache_attend(cache, q, heads, out, max_len, scale, accumulate)
     if st is not None:
         return _check(st, "mosaic_cache_attend")
