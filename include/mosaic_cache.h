@@ -10,6 +10,9 @@
  *   mosaic_cache_attend  attends from the query over the cached tokens, and
  *                        adds up how much weight each of them got,
  *   mosaic_cache_evict   drops the tokens that got least.
+ * mosaic_cache_append_norm is the first for models that normalise queries and
+ * keys head by head, and mosaic_cache_read gives cached rows back as matrices
+ * (a prompt's attention is matrix products over them).
  *
  * Conventions are those of mosaic.h (device pointers owned by the caller,
  * asynchronous on ``stream``, arguments validated before anything is
@@ -23,7 +26,8 @@
  * Slot i lies in page block_table[b * ldt + i / page_size], at place
  * i mod page_size; the row of key/value head h there starts at element
  *     page * page_stride + h * head_stride + place * token_stride
- * of ``k`` and of ``v`` and has head_dim elements. Strides are in elements.
+ * of ``k`` and of ``v`` and has head_dim elements. Strides are in elements (of
+ * a cache in 4 bits, in bytes).
  * Both orders, (page, head, place) and (page, place, head), and gaps are
  * fine, as long as the rows of a page do not overlap and pages do not.
  * Alongside every row two numbers may be kept, in contiguous arrays of
@@ -60,8 +64,23 @@ extern "C" {
 typedef enum mosaic_ftype {
   MOSAIC_F32 = 0,
   MOSAIC_BF16 = 1,
-  MOSAIC_F16 = 2
+  MOSAIC_F16 = 2,
+  MOSAIC_E2M1 = 4             /* of a cache only: 4 bits per element */
 } mosaic_ftype;
+
+/* A row of a cache in 4 bits is head_dim / 2 bytes of codes, element 2i in the
+ * low half of byte i and 2i + 1 in the high half, and head_dim / 8 bytes of
+ * scales, one for 8 elements; rounded up to 16 bytes (the rest is neither
+ * written nor read, except by eviction, which moves whole rows). A code is a
+ * sign (8) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 to 7); a scale e
+ * multiplies by 2^(e - 127), and 255 makes all 8 elements NaN. What is written:
+ * e is the smallest from 1 on that leaves no magnitude over 7 (252 at most,
+ * where magnitudes over 2^125 * 7 become 2^125 * 6), codes are the nearest, an
+ * even one between two: an element is off by at most half the distance of the
+ * codes around it (1 beyond 6), which is a fifth of the largest of its 8 or less.
+ * 8 elements with an infinity or NaN among them become NaN.
+ * The strides of such a cache are in bytes. */
+#define MOSAIC_E2M1_ROW_BYTES(head_dim) (((head_dim) / 2 + (head_dim) / 8 + 15) / 16 * 16)
 
 typedef struct mosaic_kv_cache {
   void* k;                    /* 16-byte aligned */
@@ -110,15 +129,46 @@ typedef struct mosaic_rotary {
  * is sequence b's). The i-th new token of a sequence that holds n goes to
  * slot n + i. Writes the rotated queries to q_out (rows x heads * head_dim,
  * the type of qkv, not overlapping it), rotated keys and the values into the
- * cache (rounded to its type), 0 to ``weights`` and the token's number, seen
+ * cache (rounded to its type, see there for 4 bits), 0 to ``weights`` and the token's number, seen
  * + i, to ``order`` where the cache has them, and new_state = (n, seen) plus
  * the new tokens. Tokens beyond the last slot are not kept (their queries
  * are still written). ``rotary`` NULL: nothing is rotated. x_dtype is
- * MOSAIC_F32 or the cache's type; qkv, q_out 16-byte aligned, ldx and ldq
+ * MOSAIC_F32 or the cache's type, any of the three over 4 bits; qkv, q_out 16-byte aligned, ldx and ldq
  * multiples of 16 bytes; heads a multiple of kv_heads. */
 mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv, int64_t ldx, int32_t x_dtype,
                                   int64_t rows, const int32_t* starts, int32_t heads, const mosaic_rotary* rotary,
                                   void* q_out, int64_t ldq, const int32_t* state, int32_t* new_state, void* stream);
+
+/* The same with every query and key head x normalised before it is rotated:
+ *     x_j / sqrt(mean_i x_i^2 + eps) * weight_j,
+ * the mean over the head's head_dim elements, with one weight vector for all
+ * query heads and one for all key heads. The mean and its root are computed in
+ * float64 and rounded to a float32 factor; from there on each product and sum
+ * of the element and of its rotation is rounded to float32 by itself (nothing
+ * is fused), here and wherever the cache is in 4 bits: a key between two codes
+ * takes the same one in any computation of these formulas. eps >= 0, finite. */
+typedef struct mosaic_qk_norm {
+  const float* q_weight;      /* head_dim entries each, 4-byte aligned */
+  const float* k_weight;
+  float eps;
+} mosaic_qk_norm;
+mosaic_status mosaic_cache_append_norm(const mosaic_kv_cache* cache, const void* qkv, int64_t ldx, int32_t x_dtype,
+                                       int64_t rows, const int32_t* starts, int32_t heads, const mosaic_qk_norm* norm,
+                                       const mosaic_rotary* rotary, void* q_out, int64_t ldq, const int32_t* state,
+                                       int32_t* new_state, void* stream);
+
+/* Cached tokens as rows: row t of k_out and v_out (rows x kv_heads * head_dim
+ * of out_dtype, MOSAIC_F32 or the cache's type, any of the three over 4 bits)
+ * gets the keys and values of slot first[b] + (t - starts[b]) of the sequence
+ * b with starts[b] <= t < starts[b + 1] (starts as above; NULL: row b is
+ * sequence b's; first NULL: from slot 0). Elements are rounded once where
+ * out_dtype has fewer bits than they need. A slot that holds no token (below 0,
+ * at or past lengths[b], or on a page that is not there) gives zeros. k_out and
+ * v_out 16-byte aligned, ldk and ldv multiples of 16 bytes, overlapping neither
+ * each other nor the cache. */
+mosaic_status mosaic_cache_read(const mosaic_kv_cache* cache, const int32_t* lengths, int64_t rows,
+                                const int32_t* starts, const int32_t* first, int32_t out_dtype, void* k_out,
+                                int64_t ldk, void* v_out, int64_t ldv, void* stream);
 
 /* One new token per sequence attends over its first n = min(lengths[b],
  * max_len) slots: for every query head g (key/value head h = g / (heads /
@@ -132,7 +182,7 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
  * the number of tokens may overflow there. ``accumulate`` nonzero adds p_i of
  * every head of the group to ``weights`` of slot i and head h (without atomics:
  * two runs give the same bits). q and out are batch x heads * head_dim of
- * x_dtype (MOSAIC_F32 or the cache's type), 16-byte aligned, ldq and ldo
+ * x_dtype (MOSAIC_F32 or the cache's type, any of the three over 4 bits), 16-byte aligned, ldq and ldo
  * multiples of 16 bytes, not overlapping. lengths: batch entries, e.g. the
  * first row of the state. The workspace of a call that accumulates holds every
  * score, batch x heads x max_len floats: there max_len should be no larger than

@@ -1,7 +1,8 @@
 """Cached decoding on the trusted client in float64 (numpy), from the
-definitions of include/mosaic_cache.h: rotary positions, attention of one
-token, eviction by accumulated weight. One sequence, and for the last two one
-key/value head, at a time; pages are none of its business."""
+definitions of include/mosaic_cache.h: rotary positions, norms, rows in 4 bits,
+attention of one token, eviction by accumulated weight. One sequence, and for
+attention and eviction one key/value head, at a time; pages are none of its
+business."""
 from __future__ import annotations
 
 import numpy as np
@@ -57,3 +58,55 @@ def evict(weights, order, seen, budget, recent, there=None):
     inside = {i for i in stay if i < budget}
     movers = iter(i for i in stay if i >= budget)
     return [-1 if not there[i] else i if i in inside else next(movers) for i in range(budget)]
+
+
+def normalise(x, weight, eps):
+    """x (... x dim) over its root mean square, times weight."""
+    x = np.asarray(x, dtype=np.float64)
+    return x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def row_bytes(dim):
+    return -(-(dim // 2 + dim // 8) // 16) * 16
+
+
+def to_e2m1(x):
+    """Codes (... x dim) and scales (... x dim / 8) of x: the least power of two
+    from 2^-126 to 2^125 under which no magnitude of 8 is over 7, the nearest
+    codes, an even one between two; scale 255 where one is not finite."""
+    x = np.asarray(x, dtype=np.float64)
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // 8, 8)
+    top = np.abs(g).max(axis=-1)
+    scale = np.full(top.shape, 255, dtype=np.int64)
+    fine = np.isfinite(top)
+    e = np.full(int(fine.sum()), 252)
+    for byte in range(251, 0, -1):
+        e = np.where(top[fine] <= 7.0 * 2.0 ** (byte - 127), byte, e)
+    scale[fine] = e
+    a = np.where(fine[..., None], np.abs(g), 0.0) * 2.0 ** (127.0 - np.where(fine, scale, 127))[..., None]
+    far = np.abs(a[..., None] - E2M1)
+    best = far.min(axis=-1, keepdims=True)
+    order = np.array([0, 2, 4, 6, 1, 3, 5, 7])          # even codes first
+    code = order[np.argmax(far[..., order] == best, axis=-1)] + 8 * (g < 0)
+    return np.where(fine[..., None], code, 0).reshape(x.shape), scale
+
+
+def pack_e2m1(codes, scales):
+    dim = codes.shape[-1]
+    out = np.zeros((*codes.shape[:-1], row_bytes(dim)), dtype=np.uint8)
+    out[..., : dim // 2] = codes[..., 0::2] + 16 * codes[..., 1::2]
+    out[..., dim // 2: dim // 2 + dim // 8] = scales
+    return out
+
+
+def unpack_e2m1(rows, dim):
+    """The values that rows of bytes stand for."""
+    rows = np.asarray(rows).astype(np.int64)
+    codes = np.stack([rows[..., : dim // 2] % 16, rows[..., : dim // 2] // 16], axis=-1).reshape(*rows.shape[:-1], dim)
+    scale = rows[..., dim // 2: dim // 2 + dim // 8]
+    value = E2M1[codes % 8] * np.where(codes >= 8, -1.0, 1.0)
+    factor = np.where(scale == 255, np.nan, 2.0 ** (np.where(scale == 255, 127, scale) - 127.0))
+    return (value.reshape(*rows.shape[:-1], dim // 8, 8) * factor[..., None]).reshape(*rows.shape[:-1], dim)

@@ -56,6 +56,10 @@ class MosaicRotary(ctypes.Structure):
                 ("sections", c_i32 * 4), ("interleaved", c_i32)]
 
 
+class MosaicQkNorm(ctypes.Structure):
+    _fields_ = [("q_weight", c_ptr), ("k_weight", c_ptr), ("eps", ctypes.c_float)]
+
+
 # name -> argument types (all return mosaic_status as int32 unless listed)
 _SIGNATURES = {
     "mosaic_abi_version": ([], c_i32),
@@ -94,6 +98,11 @@ _SIGNATURES = {
     "mosaic_hadamard28_rotate": ([c_ptr, c_i64, c_ptr, c_i64, c_i64, c_i64, c_ptr, c_i32, c_ptr], c_i32),
     "mosaic_cache_append": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_i32, c_i64, c_ptr, c_i32,
                              ctypes.POINTER(MosaicRotary), c_ptr, c_i64, c_ptr, c_ptr, c_ptr], c_i32),
+    "mosaic_cache_append_norm": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_i32, c_i64, c_ptr, c_i32,
+                                  ctypes.POINTER(MosaicQkNorm), ctypes.POINTER(MosaicRotary), c_ptr, c_i64, c_ptr,
+                                  c_ptr, c_ptr], c_i32),
+    "mosaic_cache_read": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_ptr, c_ptr, c_i32, c_ptr, c_i64, c_ptr,
+                           c_i64, c_ptr], c_i32),
     "mosaic_cache_attend_workspace": ([ctypes.POINTER(MosaicKvCache), c_i32, c_i64, c_i32, ctypes.POINTER(c_i64)],
                                       c_i32),
     "mosaic_cache_attend": ([ctypes.POINTER(MosaicKvCache), c_ptr, c_i64, c_i32, c_i32, c_ptr, c_i64, ctypes.c_float,

@@ -34,7 +34,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["abi.cpp", "elementwise.hip", "ring_gemm.hip", "ring_gemm_skinny.hip", "ring_gemv.hip", "hadamard.hip", "quantize.hip",
            "sparse.hip", "sparse_terms.hip", "abi_terms.cpp", "secure_input.hip", "hadamard28.hip", "probe.hip",
-           "abi_cache.cpp", "cache_append.hip", "cache_attend.hip", "cache_evict.hip"]
+           "abi_cache.cpp", "abi_cache_norm.cpp", "cache_append.hip", "cache_append_norm.hip", "cache_read.hip", "cache_attend.hip",
+           "cache_attend_e2m1.hip", "cache_evict.hip"]
 FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          # keep the compiler from forming packed fp32 instructions
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -39,10 +39,13 @@ struct Abi {
   decltype(&mosaic_cache_attend) cache_attend;
   decltype(&mosaic_cache_evict_workspace) cache_evict_workspace;
   decltype(&mosaic_cache_evict) cache_evict;
+  decltype(&mosaic_cache_append_norm) cache_append_norm;
+  decltype(&mosaic_cache_read) cache_read;
 } abi;
 
 PyObject *s_buf, *s_col0, *s_row_ptr, *s_col_idx, *s_values, *s_rows, *s_cols;   // interned attribute names
 PyObject *s_k, *s_v, *s_block_table, *s_state, *s_weights, *s_order, *s_table, *s_sections, *s_positions, *s_interleaved;
+PyObject *s_head_dim, *s_q_weight, *s_k_weight, *s_eps;
 PyObject *get_device, *get_stream;                                               // torch._C functions
 PyObject* rng_type;                                                              // the ctypes struct of mosaic_rng
 
@@ -507,6 +510,7 @@ int32_t ftype(at::ScalarType t) {
 struct Cache {
   mosaic_kv_cache c;
   at::ScalarType dtype;
+  bool four;                         // in 4 bits
   at::Device device = at::kCPU;
   int64_t slots;
   int32_t* state;
@@ -528,7 +532,8 @@ struct Cache {
     if (k == nullptr || v == nullptr || t == nullptr || st == nullptr) return false;
     if ((w == nullptr && !no_weights) || (r == nullptr && !no_order)) return false;
     c = mosaic_kv_cache{};
-    c.dtype = ftype(k->scalar_type());
+    four = k->scalar_type() == at::kByte;
+    c.dtype = four ? MOSAIC_E2M1 : ftype(k->scalar_type());
     if (c.dtype < 0 || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes() || v->strides() != k->strides() ||
         k->stride(3) != 1 || k->numel() == 0)
       return false;
@@ -542,6 +547,15 @@ struct Cache {
     c.kv_heads = (int32_t)k->size(1);
     c.page_size = (int32_t)k->size(2);
     c.head_dim = (int32_t)k->size(3);
+    if (four) {
+      int64_t dim = 0;
+      PyObject* const v = PyObject_GetAttr(o, s_head_dim);
+      const bool ok = v != nullptr && size(v, &dim) && dim <= 256 && k->size(3) >= MOSAIC_E2M1_ROW_BYTES(dim);
+      Py_XDECREF(v);
+      PyErr_Clear();
+      if (!ok) return false;
+      c.head_dim = (int32_t)dim;
+    }
     c.page_stride = k->stride(0);
     c.head_stride = k->stride(1);
     c.token_stride = k->stride(2);
@@ -558,11 +572,12 @@ struct Cache {
     slots = (int64_t)c.max_blocks * c.page_size;
     return c.k != nullptr && c.v != nullptr && c.block_table != nullptr && state != nullptr;
   }
-  // rows x cols activations: float32 or of the cache's type
+  // rows x cols activations: float32 or of the cache's type, any of the three over 4 bits
   bool rows(PyObject* o, int64_t n, int64_t cols, int32_t* type, Mat* m) const {
     const at::Tensor* t = plain(o);
-    if (t == nullptr || (t->scalar_type() != at::kFloat && t->scalar_type() != dtype)) return false;
+    if (t == nullptr || (t->scalar_type() != at::kFloat && t->scalar_type() != dtype && !four)) return false;
     *type = ftype(t->scalar_type());
+    if (*type < 0) return false;
     return matrix(o, n, cols, t->scalar_type(), false, m);
   }
   bool new_state(PyObject* o, int32_t** p) const {
@@ -577,64 +592,136 @@ struct Cache {
 
 bool heads_of(PyObject* o, int64_t* heads) { return size(o, heads) && *heads <= INT32_MAX; }
 
-// (cache, qkv, heads, q_out, starts, rotary, new_state)
-FUNCTION(cache_append, 7) {
+// Arguments of the two functions that append: cache, qkv, heads, q_out and
+// starts, and from `rest` on rotary and new_state.
+struct Append {
   Cache cache;
-  int64_t heads;
-  int32_t xt, qt;
+  int64_t heads, rows;
+  int32_t xt;
   Mat x, q, starts;
+  mosaic_rotary r{};
+  const mosaic_rotary* rotary = nullptr;
   int32_t* new_state;
   void* s;
-  NEED(cache.get(a[0]) && heads_of(a[2], &heads));
-  const at::Tensor* xten = plain(a[1]);
-  NEED(xten != nullptr && xten->dim() == 2 && xten->size(0) > 0);
-  const int64_t rows = xten->size(0), D = cache.c.head_dim;
-  NEED(cache.rows(a[1], rows, (heads + 2 * (int64_t)cache.c.kv_heads) * D, &xt, &x) &&
-       cache.rows(a[3], rows, heads * D, &qt, &q) && xt == qt);
-  if (a[4] != Py_None) {
-    const at::Tensor* t = plain(a[4]);
-    NEED(t != nullptr && t->dim() == 1 && t->size(0) == cache.c.batch + 1 && vec(a[4], cache.c.batch + 1, at::kInt, false, &starts));
-  }
-  mosaic_rotary r{};
   Ref held[2];
-  if (a[5] != Py_None) {
+  bool get(PyObject* const* a, PyObject* const* rest) {
+    int32_t qt;
+    if (!cache.get(a[0]) || !heads_of(a[2], &heads)) return false;
+    const at::Tensor* xten = plain(a[1]);
+    if (xten == nullptr || xten->dim() != 2 || xten->size(0) == 0) return false;
+    rows = xten->size(0);
+    const int64_t D = cache.c.head_dim;
+    if (!cache.rows(a[1], rows, (heads + 2 * (int64_t)cache.c.kv_heads) * D, &xt, &x) ||
+        !cache.rows(a[3], rows, heads * D, &qt, &q) || xt != qt)
+      return false;
+    if (a[4] != Py_None) {
+      const at::Tensor* t = plain(a[4]);
+      if (t == nullptr || t->dim() != 1 || t->size(0) != cache.c.batch + 1 ||
+          !vec(a[4], cache.c.batch + 1, at::kInt, false, &starts))
+        return false;
+    }
+    return (rest[0] == Py_None || rotary_of(rest[0])) && cache.new_state(rest[1], &new_state) && current_stream(&s);
+  }
+  bool rotary_of(PyObject* o) {
     bool none = false;
-    const at::Tensor *table = attr(a[5], s_table, 2, &held[0]), *positions = attr(a[5], s_positions, 2, &held[1], &none);
-    NEED(table != nullptr && table->scalar_type() == at::kFloat && table->is_contiguous() && table->size(0) > 0);
-    NEED(positions != nullptr || none);
-    PyObject* sections = PyObject_GetAttr(a[5], s_sections);
+    const at::Tensor *table = attr(o, s_table, 2, &held[0]), *positions = attr(o, s_positions, 2, &held[1], &none);
+    if (table == nullptr || table->scalar_type() != at::kFloat || !table->is_contiguous() || table->size(0) == 0) return false;
+    if (positions == nullptr && !none) return false;
+    PyObject* sections = PyObject_GetAttr(o, s_sections);
     int64_t pairs = 0;
     bool ok = sections != nullptr && (PyList_CheckExact(sections) || PyTuple_CheckExact(sections));
     const Py_ssize_t axes = ok ? PySequence_Fast_GET_SIZE(sections) : 0;
     ok = ok && axes >= 1 && axes <= 4;
     for (Py_ssize_t i = 0; ok && i < axes; ++i) {
       int64_t n;
-      ok = integer(PySequence_Fast_GET_ITEM(sections, i), &n) && n >= 0 && n <= D;
+      ok = integer(PySequence_Fast_GET_ITEM(sections, i), &n) && n >= 0 && n <= cache.c.head_dim;
       if (ok) r.sections[i] = (int32_t)n;
       pairs += ok ? n : 0;
     }
     Py_XDECREF(sections);
     PyErr_Clear();
-    NEED(ok && table->size(1) == 2 * pairs);
-    PyObject* flag = PyObject_GetAttr(a[5], s_interleaved);
+    if (!ok || table->size(1) != 2 * pairs) return false;
+    PyObject* flag = PyObject_GetAttr(o, s_interleaved);
     ok = flag != nullptr && truth(flag, &r.interleaved);
     Py_XDECREF(flag);
     PyErr_Clear();
-    NEED(ok);
+    if (!ok) return false;
     if (positions != nullptr) {
-      NEED(positions->scalar_type() == at::kInt && positions->size(0) >= axes && positions->size(1) >= rows &&
-           (rows == 1 || positions->stride(1) == 1));
+      if (positions->scalar_type() != at::kInt || positions->size(0) < axes || positions->size(1) < rows ||
+          (rows > 1 && positions->stride(1) != 1))
+        return false;
       r.positions = (const int32_t*)positions->data_ptr();
       r.ldp = axes > 1 ? positions->stride(0) : rows;
     }
     r.table = (const float*)table->data_ptr();
     r.rows = table->size(0);
     r.naxes = (int32_t)axes;
+    rotary = &r;
+    return true;
   }
-  NEED(cache.new_state(a[6], &new_state) && current_stream(&s));
+};
+
+// (cache, qkv, heads, q_out, starts, rotary, new_state)
+FUNCTION(cache_append, 7) {
+  Append p;
+  NEED(p.get(a, a + 5));
   return status([&] {
-    return abi.cache_append(&cache.c, x.p, x.ld, xt, rows, (const int32_t*)starts.p, (int32_t)heads,
-                            a[5] != Py_None ? &r : nullptr, q.p, q.ld, cache.state, new_state, s);
+    return abi.cache_append(&p.cache.c, p.x.p, p.x.ld, p.xt, p.rows, (const int32_t*)p.starts.p, (int32_t)p.heads,
+                            p.rotary, p.q.p, p.q.ld, p.cache.state, p.new_state, p.s);
+  });
+}
+
+// (cache, qkv, heads, q_out, norm, starts, rotary, new_state)
+FUNCTION(cache_append_norm, 8) {
+  Append p;
+  PyObject* const first[] = {a[0], a[1], a[2], a[3], a[5]};
+  NEED(p.get(first, a + 6));
+  Ref held[2];
+  mosaic_qk_norm norm{};
+  const at::Tensor *qw = attr(a[4], s_q_weight, 1, &held[0]), *kw = attr(a[4], s_k_weight, 1, &held[1]);
+  for (const at::Tensor* w : {qw, kw})
+    NEED(w != nullptr && w->scalar_type() == at::kFloat && w->size(0) == p.cache.c.head_dim && w->stride(0) == 1);
+  PyObject* const eps = PyObject_GetAttr(a[4], s_eps);
+  const bool ok = eps != nullptr && PyFloat_CheckExact(eps);
+  if (ok) norm.eps = (float)PyFloat_AS_DOUBLE(eps);
+  Py_XDECREF(eps);
+  PyErr_Clear();
+  NEED(ok);
+  norm.q_weight = (const float*)qw->data_ptr();
+  norm.k_weight = (const float*)kw->data_ptr();
+  return status([&] {
+    return abi.cache_append_norm(&p.cache.c, p.x.p, p.x.ld, p.xt, p.rows, (const int32_t*)p.starts.p, (int32_t)p.heads,
+                                 &norm, p.rotary, p.q.p, p.q.ld, p.cache.state, p.new_state, p.s);
+  });
+}
+
+// (cache, k_out, v_out, starts, first)
+FUNCTION(cache_read, 5) {
+  Cache cache;
+  int32_t kt, vt;
+  Mat k, v, starts, first;
+  void* s;
+  NEED(cache.get(a[0]));
+  const at::Tensor* kten = plain(a[1]);
+  const at::Tensor* vten = plain(a[2]);
+  NEED(kten != nullptr && vten != nullptr && kten->dim() == 2 && vten->dim() == 2 && kten->size(0) > 0 &&
+       vten->size(0) == kten->size(0));
+  const int64_t rows = kten->size(0), width = (int64_t)cache.c.kv_heads * cache.c.head_dim;
+  NEED(cache.rows(a[1], rows, width, &kt, &k) && cache.rows(a[2], rows, width, &vt, &v) && kt == vt);
+  const struct {
+    PyObject* o;
+    int64_t n;
+    Mat* m;
+  } lists[] = {{a[3], (int64_t)cache.c.batch + 1, &starts}, {a[4], cache.c.batch, &first}};
+  for (const auto& l : lists)
+    if (l.o != Py_None) {
+      const at::Tensor* t = plain(l.o);
+      NEED(t != nullptr && t->dim() == 1 && t->size(0) == l.n && vec(l.o, l.n, at::kInt, false, l.m));
+    }
+  NEED(current_stream(&s));
+  return status([&] {
+    return abi.cache_read(&cache.c, cache.state, rows, (const int32_t*)starts.p, (const int32_t*)first.p, kt, k.p, k.ld,
+                          v.p, v.ld, s);
   });
 }
 
@@ -738,7 +825,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {METHOD(bind), METHOD(sample), METHOD(mask), METHOD(masked_matmul), METHOD(integrity_check),
                          METHOD(unmask), METHOD(unmask_words), METHOD(rotate_quantize_mask), METHOD(hadamard_rotate),
                          METHOD(quantize_rows), METHOD(stream_terms), METHOD(cols_terms), METHOD(cache_append),
-                         METHOD(cache_attend), METHOD(cache_evict), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(cache_attend), METHOD(cache_evict), METHOD(cache_append_norm), METHOD(cache_read), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -752,10 +839,12 @@ PyMODINIT_FUNC PyInit__binding(void) {
   s_rows = PyUnicode_InternFromString("rows");
   s_cols = PyUnicode_InternFromString("cols");
   PyObject** const names[] = {&s_k,     &s_v,     &s_block_table, &s_state,     &s_weights,
-                              &s_order, &s_table, &s_sections,    &s_positions, &s_interleaved};
+                              &s_order, &s_table, &s_sections,    &s_positions, &s_interleaved,
+                              &s_head_dim, &s_q_weight, &s_k_weight, &s_eps};
   const char* const texts[] = {"k",     "v",     "block_table", "state",     "weights",
-                               "order", "table", "sections",    "positions", "interleaved"};
-  for (int i = 0; i < 10; ++i)
+                               "order", "table", "sections",    "positions", "interleaved",
+                               "head_dim", "q_weight", "k_weight", "eps"};
+  for (int i = 0; i < 14; ++i)
     if ((*names[i] = PyUnicode_InternFromString(texts[i])) == nullptr) return nullptr;
   if (!s_buf || !s_col0 || !s_row_ptr || !s_col_idx || !s_values || !s_rows || !s_cols) return nullptr;
   return PyModule_Create(&module);

@@ -24,6 +24,13 @@ struct CacheView {
   int32_t dtype;
 };
 
+// Normalisation of queries and keys.
+struct NormView {
+  const float* q_weight;    // null: none
+  const float* k_weight;
+  double eps;
+};
+
 constexpr int kMaxAxes = 4;
 struct RotaryView {
   const float* table;       // null: no rotation
@@ -38,6 +45,7 @@ struct RotaryView {
 struct AppendLaunch {
   CacheView c;
   RotaryView rot;
+  NormView norm;
   const void* x;
   void* q;
   int64_t ldx, ldq;         // bytes
@@ -49,6 +57,21 @@ struct AppendLaunch {
   int32_t* new_state;
 };
 hipError_t launch_cache_append(const AppendLaunch& a, hipStream_t s);
+// The kernel of calls with norms or a cache in 4 bits.
+void launch_cache_append_norm(const AppendLaunch& a, hipStream_t s);
+
+struct ReadLaunch {
+  CacheView c;
+  const int32_t* lengths;
+  int64_t rows;
+  const int32_t* starts;
+  const int32_t* first;
+  int32_t out_dtype;
+  void* k;
+  void* v;
+  int64_t ldk, ldv;         // bytes
+};
+hipError_t launch_cache_read(const ReadLaunch& a, hipStream_t s);
 
 struct AttendLaunch {
   CacheView c;
@@ -65,6 +88,8 @@ struct AttendLaunch {
 };
 int64_t cache_attend_workspace(const CacheView& c, int32_t heads, int64_t max_len, int32_t accumulate);
 hipError_t launch_cache_attend(const AttendLaunch& a, hipStream_t s);
+// The same over a cache in 4 bits.
+hipError_t launch_cache_attend_e2m1(const AttendLaunch& a, hipStream_t s);
 
 struct EvictLaunch {
   CacheView c;
@@ -81,6 +106,17 @@ int64_t cache_evict_workspace(const CacheView& c, int64_t max_len, int64_t budge
 hipError_t launch_cache_evict(const EvictLaunch& a, hipStream_t s);
 
 #ifdef __HIPCC__
+
+// The sequence that row t belongs to: the last b < batch with starts[b] <= t.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int64_t t) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (starts[mid] <= t) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
 
 // Element types of activations and cache rows by mosaic_ftype.
 template <int FT> struct FloatType;

@@ -9,18 +9,10 @@
 // bound by that traffic: 4096 tokens of 64 + 2 * 8 heads of 128 floats in 61 us
 // (5.5 TB/s). A single token takes 3.3 us and 48 take 3.7 us, the latency of
 // launch, state, page and table; its row is asked for before these.
-#include "cache.h"
-#include "device_common.h"
-#include "dispatch.h"
+#include "cache_append.h"
 
 namespace mosaic {
 namespace {
-
-constexpr int kFewRows = 256;     // no more than one workgroup per compute unit
-// Rows that the 32 MiB of second-level cache cannot hold pass by it (168 MB of
-// q|k|v: 61 us, 69 us through it); fewer are left there for the attention that
-// comes next.
-constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 
 // How the elements of a pair lie. A thread works on V consecutive elements
 // (16 bytes of the row).
@@ -30,46 +22,9 @@ enum RotaryMode {
   ROT_NEIGHBOURS      // 2j and 2j + 1 (and P = 0, nothing rotated): a chunk holds whole pairs
 };
 
-// The sequence that row t belongs to: the last b < batch with starts[b] <= t.
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int64_t t) {
-  int lo = 0, hi = batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (starts[mid] <= t) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-// (held, seen) of sequence b after n new tokens.
-__device__ __forceinline__ void advance(const AppendLaunch& a, int b, int32_t n, int64_t slots) {
-  const int64_t held = (int64_t)held_tokens(a.state, b, slots) + n;
-  const int32_t seen = a.state[a.c.batch + b];
-  a.new_state[b] = (int32_t)(held < slots ? held : slots);
-  a.new_state[a.c.batch + b] = (int32_t)((uint32_t)seen + (uint32_t)n);
-}
-
-__device__ __forceinline__ int32_t fresh_tokens(const AppendLaunch& a, int b) {
-  if (a.starts == nullptr) return 1;
-  const int64_t n = (int64_t)a.starts[b + 1] - a.starts[b];
-  return n < 0 ? 0 : n > a.rows ? (int32_t)a.rows : (int32_t)n;
-}
-
 __global__ __launch_bounds__(256) void cache_advance_kernel(AppendLaunch a) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   if (b < a.c.batch) advance(a, b, fresh_tokens(a, b), (int64_t)a.c.max_blocks << a.c.log2_page);
-}
-
-template <class T, int V> struct alignas(sizeof(T) * V) Chunk { T e[V]; };
-
-// STREAM: past the caches.
-template <bool STREAM, class T> __device__ __forceinline__ T load_piece(const char* p) {
-  if constexpr (STREAM) return __builtin_bit_cast(T, __builtin_nontemporal_load((const u32x4*)p));
-  else return *(const T*)p;
-}
-template <bool STREAM, class T> __device__ __forceinline__ void store_piece(char* p, T v) {
-  if constexpr (STREAM && sizeof(T) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-  else *(T*)p = v;
 }
 
 // Where a chunk of a head goes: q_out, or the head's row of k or v.
@@ -224,7 +179,8 @@ void launch_types(const AppendLaunch& a, hipStream_t s) {
 
 hipError_t launch_cache_append(const AppendLaunch& a, hipStream_t s) {
   if (a.rows > 0) {
-    if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_F32) launch_types<MOSAIC_F32, MOSAIC_F32>(a, s);
+    if (a.norm.q_weight != nullptr || a.c.dtype == MOSAIC_E2M1) launch_cache_append_norm(a, s);
+    else if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_F32) launch_types<MOSAIC_F32, MOSAIC_F32>(a, s);
     else if (a.x_dtype == MOSAIC_F32 && a.c.dtype == MOSAIC_BF16) launch_types<MOSAIC_F32, MOSAIC_BF16>(a, s);
     else if (a.x_dtype == MOSAIC_F32) launch_types<MOSAIC_F32, MOSAIC_F16>(a, s);
     else if (a.c.dtype == MOSAIC_BF16) launch_types<MOSAIC_BF16, MOSAIC_BF16>(a, s);

@@ -521,7 +521,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(EvictLaunch a, int64_t 
   if (moves == 0) return;
   const Lists l = lists_of(a, moves, bh);
   const int32_t all = *l.count;
-  const int32_t chunks = a.c.head_dim * (a.c.dtype == MOSAIC_F32 ? 4 : 2) / 16;
+  const int32_t chunks = a.c.dtype == MOSAIC_E2M1 ? MOSAIC_E2M1_ROW_BYTES(a.c.head_dim) / 16
+                                                  : a.c.head_dim * (a.c.dtype == MOSAIC_F32 ? 4 : 2) / 16;
   for (int32_t first = (int32_t)blockIdx.x * kMovesPerBlock; first < all; first += (int32_t)gridDim.x * kMovesPerBlock) {
     const int32_t count = min(all - first, kMovesPerBlock);
     for (int32_t w = threadIdx.x; w < count * chunks; w += 256) {

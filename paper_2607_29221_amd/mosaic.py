@@ -45,7 +45,7 @@ _BOUND = ("mosaic_sample", "mosaic_mask", "mosaic_masked_matmul", "mosaic_integr
           "mosaic_unmask_words", "mosaic_rotate_quantize_mask", "mosaic_sparse_stream_gather_rows_terms",
           "mosaic_sparse_gather_cols_terms", "mosaic_sparse_gather_cols", "mosaic_hadamard_rotate", "mosaic_quantize_rows",
           "mosaic_cache_append", "mosaic_cache_attend_workspace", "mosaic_cache_attend",
-          "mosaic_cache_evict_workspace", "mosaic_cache_evict")
+          "mosaic_cache_evict_workspace", "mosaic_cache_evict", "mosaic_cache_append_norm", "mosaic_cache_read")
 _b = None
 
 
@@ -527,27 +527,35 @@ class KVCache:
     batch x blocks) holds every sequence's pages, ``state`` (int32, 2 x batch)
     how many tokens it holds and how many it has seen. ``weights`` (float32)
     and ``order`` (int32), contiguous (pages, kv_heads, page_size), are needed
-    for eviction only."""
+    for eviction only. In 4 bits (uint8 tensors) the last dimension is a row's
+    bytes, row_bytes(head_dim) or more, and ``head_dim`` must be given."""
     k: torch.Tensor
     v: torch.Tensor
     block_table: torch.Tensor
     state: torch.Tensor
     weights: Optional[torch.Tensor] = None
     order: Optional[torch.Tensor] = None
+    head_dim: Optional[int] = None
+
+    @staticmethod
+    def row_bytes(head_dim: int) -> int:
+        """Bytes of a row in 4 bits."""
+        return (head_dim // 2 + head_dim // 8 + 15) // 16 * 16
 
     @staticmethod
     def empty(batch: int, max_len: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, page_size: int = 64,
               evicts: bool = False, device="cuda") -> "KVCache":
         """A cache without tokens, with pages of its own for ``max_len`` slots
-        of each sequence."""
+        of each sequence; ``dtype`` torch.uint8: in 4 bits."""
         blocks = (max_len + page_size - 1) // page_size
         pages = batch * blocks
-        k = torch.empty((pages, kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        width = KVCache.row_bytes(head_dim) if dtype == torch.uint8 else head_dim
+        k = torch.empty((pages, kv_heads, page_size, width), dtype=dtype, device=device)
         table = torch.arange(pages, dtype=torch.int32, device=device).reshape(batch, blocks)
         state = torch.zeros((2, batch), dtype=torch.int32, device=device)
         weights = torch.zeros(k.shape[:3], device=device) if evicts else None
         order = torch.zeros(k.shape[:3], dtype=torch.int32, device=device) if evicts else None
-        return KVCache(k, torch.empty_like(k), table, state, weights, order)
+        return KVCache(k, torch.empty_like(k), table, state, weights, order, head_dim)
 
     @property
     def batch(self) -> int:
@@ -579,7 +587,17 @@ class Rotary:
         return torch.cat([a.cos(), a.sin()], dim=1).float()
 
 
+@dataclass
+class QKNorm:
+    """Norms of queries and keys, head by head: x / sqrt(mean x^2 + eps) times
+    ``q_weight`` or ``k_weight`` (float32, head_dim entries)."""
+    q_weight: torch.Tensor
+    k_weight: torch.Tensor
+    eps: float = 1e-6
+
+
 _FTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_CACHE_FTYPE = {**_FTYPE, torch.uint8: 4}
 
 
 def _device_tensor(t, name: str, dtypes, dim: int) -> None:
@@ -594,8 +612,8 @@ def _device_tensor(t, name: str, dtypes, dim: int) -> None:
 def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
     """The C struct of a cache whose tensors fit together."""
     k, v, table = cache.k, cache.v, cache.block_table
-    _device_tensor(k, "cache.k", _FTYPE, 4)
-    _device_tensor(v, "cache.v", _FTYPE, 4)
+    _device_tensor(k, "cache.k", _CACHE_FTYPE, 4)
+    _device_tensor(v, "cache.v", _CACHE_FTYPE, 4)
     if v.dtype != k.dtype or v.shape != k.shape or v.stride() != k.stride():
         raise ValueError("cache.k and cache.v must have the same type, shape and strides")
     if k.stride(3) != 1:
@@ -613,16 +631,20 @@ def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
             if t.shape != k.shape[:3] or not t.is_contiguous():
                 raise ValueError(f"cache.{name} must be a contiguous (pages, kv_heads, page_size) tensor")
     pages, heads, page, dim = k.shape
+    if k.dtype == torch.uint8:
+        if cache.head_dim is None or dim < KVCache.row_bytes(cache.head_dim):
+            raise ValueError("a cache in 4 bits needs its head_dim, and rows of KVCache.row_bytes(head_dim)")
+        dim = cache.head_dim
     # a single row's stride has no meaning; 0 is a table that all sequences share
     return _lib.MosaicKvCache(k=_ptr(k), v=_ptr(v), weights=_ptr(cache.weights), order=_ptr(cache.order),
                               block_table=_ptr(table), ldt=table.stride(0) if batch > 1 else blocks, pages=pages,
                               page_stride=k.stride(0), head_stride=k.stride(1), token_stride=k.stride(2),
-                              dtype=_FTYPE[k.dtype], batch=batch, max_blocks=blocks, kv_heads=heads, head_dim=dim,
+                              dtype=_CACHE_FTYPE[k.dtype], batch=batch, max_blocks=blocks, kv_heads=heads, head_dim=dim,
                               page_size=page)
 
 
 def _cache_rows(t: torch.Tensor, rows: int, cols: int, name: str, cache: KVCache) -> None:
-    _device_tensor(t, name, (torch.float32, cache.k.dtype), 2)
+    _device_tensor(t, name, _FTYPE if cache.k.dtype == torch.uint8 else (torch.float32, cache.k.dtype), 2)
     if t.shape[0] < rows or t.shape[1] < cols:
         raise ValueError(f"{name} is {tuple(t.shape)}, needs at least ({rows}, {cols})")
     if t.stride(1) != 1:
@@ -640,16 +662,10 @@ def _same_shape(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: s
     return t
 
 
-def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Tensor,
-                        starts: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
-                        new_state: Optional[torch.Tensor] = None) -> None:
-    """New tokens, one per row of qkv (queries, keys, values of ``heads`` and
-    kv_heads heads): rotated queries to q_out, rotated keys and values into
-    the cache. Rows starts[b] .. starts[b + 1] - 1 are sequence b's (None: row
-    b). The state is advanced in place unless new_state is given."""
-    st = (_b or _native()).cache_append(cache, qkv, heads, q_out, starts, rotary, new_state)
-    if st is not None:
-        return _check(st, "mosaic_cache_append")
+def _append_args(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Tensor, starts: Optional[torch.Tensor],
+                 rotary: Optional[Rotary], new_state: Optional[torch.Tensor]):
+    """Checked arguments of the two functions that append: what comes before the
+    norm, the rotary positions, and what comes after them."""
     c = _cache_arg(cache)
     rows = qkv.shape[0]
     _cache_rows(qkv, rows, (heads + 2 * c.kv_heads) * c.head_dim, "qkv", cache)
@@ -679,10 +695,66 @@ def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: to
         r = _lib.MosaicRotary(table=_ptr(rotary.table), rows=rotary.table.shape[0], positions=_ptr(rotary.positions), ldp=ldp,
                               naxes=len(sections), sections=(ctypes.c_int32 * 4)(*sections),
                               interleaved=1 if rotary.interleaved else 0)
-    _check(_lib.load().mosaic_cache_append(ctypes.byref(c), _ptr(qkv), qkv.stride(0), _FTYPE[qkv.dtype], rows,
-                                           _ptr(starts), heads, None if r is None else ctypes.byref(r), _ptr(q_out),
-                                           q_out.stride(0), _ptr(cache.state), _ptr(state), _stream()),
-           "mosaic_cache_append")
+    return ((ctypes.byref(c), _ptr(qkv), qkv.stride(0), _FTYPE[qkv.dtype], rows, _ptr(starts), heads),
+            None if r is None else ctypes.byref(r),
+            (_ptr(q_out), q_out.stride(0), _ptr(cache.state), _ptr(state), _stream()))
+
+
+def mosaic_cache_append(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Tensor,
+                        starts: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                        new_state: Optional[torch.Tensor] = None) -> None:
+    """New tokens, one per row of qkv (queries, keys, values of ``heads`` and
+    kv_heads heads): rotated queries to q_out, rotated keys and values into
+    the cache. Rows starts[b] .. starts[b + 1] - 1 are sequence b's (None: row
+    b). The state is advanced in place unless new_state is given."""
+    st = (_b or _native()).cache_append(cache, qkv, heads, q_out, starts, rotary, new_state)
+    if st is not None:
+        return _check(st, "mosaic_cache_append")
+    before, r, after = _append_args(cache, qkv, heads, q_out, starts, rotary, new_state)
+    _check(_lib.load().mosaic_cache_append(*before, r, *after), "mosaic_cache_append")
+
+
+def mosaic_cache_append_norm(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Tensor, norm: QKNorm,
+                             starts: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                             new_state: Optional[torch.Tensor] = None) -> None:
+    """mosaic_cache_append with every query and key head normalised before it is
+    rotated."""
+    st = (_b or _native()).cache_append_norm(cache, qkv, heads, q_out, norm, starts, rotary, new_state)
+    if st is not None:
+        return _check(st, "mosaic_cache_append_norm")
+    before, r, after = _append_args(cache, qkv, heads, q_out, starts, rotary, new_state)
+    dim = cache.head_dim if cache.k.dtype == torch.uint8 else cache.k.shape[3]
+    for name, w in (("q_weight", norm.q_weight), ("k_weight", norm.k_weight)):
+        _device_tensor(w, f"norm.{name}", (torch.float32,), 1)
+        if w.shape[0] != dim or not w.is_contiguous():
+            raise ValueError(f"norm.{name} must be a contiguous vector of head_dim entries")
+    w = _lib.MosaicQkNorm(q_weight=_ptr(norm.q_weight), k_weight=_ptr(norm.k_weight), eps=norm.eps)
+    _check(_lib.load().mosaic_cache_append_norm(*before, ctypes.byref(w), r, *after), "mosaic_cache_append_norm")
+
+
+def mosaic_cache_read(cache: KVCache, k_out: torch.Tensor, v_out: torch.Tensor, starts: Optional[torch.Tensor] = None,
+                      first: Optional[torch.Tensor] = None) -> None:
+    """Cached tokens as rows of kv_heads * head_dim: rows starts[b] ..
+    starts[b + 1] - 1 of k_out and v_out get slots first[b], first[b] + 1, ...
+    of sequence b (starts None: row b is sequence b's; first None: from slot 0),
+    zeros where a slot holds no token."""
+    st = (_b or _native()).cache_read(cache, k_out, v_out, starts, first)
+    if st is not None:
+        return _check(st, "mosaic_cache_read")
+    c = _cache_arg(cache)
+    rows, width = k_out.shape[0], c.kv_heads * c.head_dim
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        _cache_rows(t, rows, width, name, cache)
+    if v_out.dtype != k_out.dtype or v_out.shape[0] != rows:
+        raise ValueError("k_out and v_out must have the same type and as many rows")
+    for name, t, n in (("starts", starts, c.batch + 1), ("first", first, c.batch)):
+        if t is not None:
+            _device_tensor(t, name, _INT, 1)
+            if t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+                raise ValueError(f"{name} must be a contiguous vector of {n} entries")
+    _check(_lib.load().mosaic_cache_read(ctypes.byref(c), _ptr(cache.state), rows, _ptr(starts), _ptr(first),
+                                         _FTYPE[k_out.dtype], _ptr(k_out), k_out.stride(0), _ptr(v_out), v_out.stride(0),
+                                         _stream()), "mosaic_cache_read")
 
 
 def mosaic_cache_attend(cache: KVCache, q: torch.Tensor, heads: int, out: torch.Tensor,
