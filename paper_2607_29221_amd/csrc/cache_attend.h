@@ -103,7 +103,7 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // once, since a unit with two takes twice as long (12 key/value heads: 249 us
   // with 264, 173 us with 252), but more per unit where more than one unit in 16
   // would idle (71 heads: 217 us with 213, 186 us with 497).
-  int32_t slots = p.tile_groups > 1 && c.head_dim <= 128 ? 512 : 256;
+  int32_t slots = c.dtype == MOSAIC_E2M1 ? 512 : p.tile_groups > 1 && c.head_dim <= 128 ? 512 : 256;
   int64_t wanted;
   while (true) {
     const int64_t shares = p.tile_groups > 1 ? slots / kXcds / p.tile_groups * kXcds : slots;

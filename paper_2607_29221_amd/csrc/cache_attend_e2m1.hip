@@ -17,6 +17,7 @@
 //   8 tokens, a dword of codes and a scale byte each, and turns them with byte
 //   permutes once they are bf16.
 #include <cfloat>
+#include <type_traits>
 
 #include "cache_attend.h"
 #include "e2m1.h"
@@ -55,34 +56,82 @@ template <int PARTS> __device__ __forceinline__ void split_query(float x, __bf16
   }
 }
 
-constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : NT == 2 ? 2 : 3; }
+// Rows come to LDS as they lie, 16 bytes per lane and load: lane l of the wave
+// writes LDS bytes [to + 16 l, to + 16 l + 16), zeros for what lies past the
+// descriptor's range. In assembly, so that the compiler does not wait for all
+// loads before each read of LDS; a wave waits for its own with landed().
+// Nothing else in this kernel uses M0.
+typedef int v4i __attribute__((ext_vector_type(4)));
+template <bool STREAM> __device__ __forceinline__ void row_load(v4i rsrc, uint32_t to, int off) {
+  if constexpr (STREAM)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(off), "s"(rsrc) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rsrc) : "memory");
+}
+// At most N of the wave's vector-memory accesses are under way.
+template <int N> __device__ __forceinline__ void landed() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
-// NT: blocks of 16 query heads per wave; STREAM: past the caches (cache_attend.hip).
-template <int XT, int DP, int NT, bool STREAM>
+constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : 2; }
+
+// Weights as bf16 parts, two to a dword.
+template <int PARTS> __device__ __forceinline__ void split_pair(float x, float y, uint32_t* part) {
+#pragma unroll
+  for (int s = 0; s < PARTS; ++s) {
+    bf16x2 r;
+    r[0] = (__bf16)x;
+    r[1] = (__bf16)y;
+    part[s] = __builtin_bit_cast(uint32_t, r);
+    x -= __uint_as_float(part[s] << 16);
+    y -= __uint_as_float(part[s] & 0xFFFF0000u);
+  }
+}
+
+// Bytes of LDS: operands of the first product by lane; the waves' stages of rows;
+// where weights are added up, scores on their way to memory. The waves' outputs
+// come over these at the end.
+template <int XT, int DP, int NT> struct Lds {
+  typedef Form<XT, DP> F;
+  static constexpr int kStages = 2;             // of a wave, kTokens rows of keys and of values each
+  static constexpr int kStageBytes = 2 * F::kTokens * MOSAIC_E2M1_ROW_BYTES(DP);
+  static constexpr int kQuery = NT * F::kParts * F::kKeyDwords * 64 * 16;
+  static constexpr int kRows = kWaves * kStages * kStageBytes;
+  static constexpr int kPast = 256;             // columns past head_dim are read from what follows a row
+  static constexpr int kHold = 128 * NT;        // of a wave's scores, 16 bytes each: one step's at least
+  static constexpr int kSlab = kWaves * kHeadTile * (DP + 4) * 4;
+  static constexpr int bytes(bool accumulate) {
+    const int in = kQuery + kRows + kPast + (accumulate ? kWaves * kHold * 16 : 0);
+    return in > kSlab ? in : kSlab;
+  }
+};
+
+// NT: blocks of 16 query heads per wave. FULL: head_dim is DP. STREAM: past the
+// caches, as no other workgroup reads the same rows.
+template <int XT, int DP, int NT, bool FULL, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2m1_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef Form<XT, DP> F;
+  typedef Lds<XT, DP, NT> S;
   typedef typename F::X X;
   typedef bf16x8 Frag;
   constexpr int KL = F::kKeyDwords, NV = F::kValuePieces, EV = F::kEach, PARTS = F::kParts, WPARTS = F::kWeightParts;
-  constexpr int kPolicy = STREAM ? kStream : 0;
-  constexpr int kHold = 8192 / 16;              // of a wave's scores, 16 bytes each
-  union Shared {
-    struct {
-      Frag query[NT][PARTS][KL][64];            // operands of the first product, by lane
-      f32x4 held[kWaves][kHold];                // scores on their way to memory
-    } in;
-    float slab[kWaves][kHeadTile][DP + 4];      // outputs of the waves, at the end
-  };
-  __shared__ Shared shared;
+  constexpr int kHold = S::kHold, kStages = S::kStages, kStageBytes = S::kStageBytes;
+  constexpr int kMostLoads = (2 * MOSAIC_E2M1_ROW_BYTES(DP) / 16 + 3) / 4;   // per 32 rows
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float stat[NT][kWaves][kHeadTile][2];
+  Frag(*query)[PARTS][KL][64] = (Frag(*)[PARTS][KL][64])lds;
+  float(*slab)[kHeadTile][DP + 4] = (float(*)[kHeadTile][DP + 4])lds;
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char* const rows = lds + S::kQuery + wave * kStages * kStageBytes;
+  f32x4* const held = (f32x4*)(lds + S::kQuery + S::kRows + S::kPast) + wave * kHold;
   const uint32_t share_of = blockIdx.y * kXcds + blockIdx.x % kXcds;
   const int u = share_of / (uint32_t)a.c.kv_heads, h = share_of - u * a.c.kv_heads;
   const int tile0 = blockIdx.x / kXcds * NT;
   if (u >= workgroups) return;
-  const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
+  const int group = a.heads / a.c.kv_heads, D = FULL ? DP : a.c.head_dim;
 
   int before;
   FirstSteps first64;
@@ -115,84 +164,86 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           raw[nt][c][l] = *(const u32x4*)(row + min(((own_lane >> 4) * KL + c) * 8, D - 8) * (int)sizeof(X) + 16 * l);
     }
 
-    // a lane's offsets within a block of 16 rows; columns past head_dim lie nowhere
-    const int ts = (int)a.c.token_stride;
-    const int key_off = quad * KL * 8 < D ? col * ts + quad * KL * 4 : kNowhere;
-    const int key_scale = quad * KL * 8 < D ? col * ts + D / 2 + quad * KL : kNowhere;
-    uint32_t there[KL];                         // all bits of the dwords of the row, none past it
+    // Offsets of the lane's 16 bytes of a block's rows. 32 rows are a block where
+    // they lie in one page, 16 otherwise.
+    const int ts = (int)a.c.token_stride, row_bytes = MOSAIC_E2M1_ROW_BYTES(D), pieces = row_bytes / 16;
+    const bool wide = a.c.log2_page > 4;
+    const int row_loads = wide ? (2 * pieces + 3) / 4 : (pieces + 3) / 4;
+    int row_off[kMostLoads];
 #pragma unroll
-    for (int c = 0; c < KL; ++c) there[c] = (quad * KL + c) * 8 < D ? ~0u : 0u;
-    int value_off[NV], value_scale[NV];
+    for (int j = 0; j < kMostLoads; ++j) row_off[j] = (64 * j + lane) / pieces * ts + (64 * j + lane) % pieces * 16;
+    // a scale's exponent bits, none of those past the row (codes there meet queries of 0)
+    uint32_t there[KL];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int d = (16 * v + col) * EV;
-      value_off[v] = d < D ? 4 * quad * ts + d / 2 : kNowhere;
-      value_scale[v] = d < D ? 4 * quad * ts + D / 2 + d / 8 : kNowhere;
-    }
+    for (int c = 0; c < KL; ++c) there[c] = (quad * KL + c) * 8 < D ? 0x7F800000u : 0u;
 
-    // a block of 16 tokens: its first row's place in memory and how many there are
-    struct Block {
-      int64_t base;
-      int valid;
-    };
+    // the page of a slot, as the table has it (of a later one than the last, the
+    // last one's), and how many tokens of 16 or 32 from there on there are
     const int page_mask = (1 << a.c.log2_page) - 1;
-    auto block_at = [&](int slot) {
-      Block k = {0, 0};
-      if (slot < t1) {
-        const int page = page_of_uniform(a.c, b, slot);
-        if (page >= 0) {
-          k.base = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (slot & page_mask) * ts;
-          k.valid = min(t1 - slot, 16);
-        }
-      }
-      return k;
+    const uniform_i32 pages = (uniform_i32)(uintptr_t)a.c.table + b * a.c.ldt;
+    auto page_at = [&](int slot) { return pages[min(slot, t1 - 1) >> a.c.log2_page]; };
+    auto valid_at = [&](int slot, int page, int most) {
+      return (uint32_t)page < (uint32_t)a.c.pages ? max(min(t1 - slot, most), 0) : 0;
     };
-    uint32_t key[F::kSub][KL], key_e[F::kSub][(KL + 3) / 4];
-    auto load_keys = [&](const Block* k) {
-#pragma unroll
-      for (int s = 0; s < F::kSub; ++s) {
-        const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.k + k[s].base, k[s].valid * ts);
-        if constexpr (KL == 2) {
-          const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, key_off, 0, kPolicy));
-          key[s][0] = w[0];
-          key[s][1] = w[1];
-          key_e[s][0] = __builtin_amdgcn_raw_buffer_load_b16(r, key_scale, 0, kPolicy);
-        } else {
-#pragma unroll
-          for (int c = 0; c < KL / 4; ++c) {
-            // (of 256: the second 16 bytes may lie past the row)
-            const bool in = quad * KL * 8 + 32 * c < D;
-            const u32x4 w = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, c == 0 || in ? key_off + 16 * c : kNowhere, 0, kPolicy));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) key[s][4 * c + i] = w[i];
-            key_e[s][c] = __builtin_amdgcn_raw_buffer_load_b32(r, c == 0 || in ? key_scale + 4 * c : kNowhere, 0, kPolicy);
-          }
-        }
-      }
-    };
+    const char *const head_k = a.c.k + (int64_t)h * a.c.head_stride, *const head_v = a.c.v + (int64_t)h * a.c.head_stride;
     constexpr int kStep = F::kTokens * kWaves;
     const int first = t0 + F::kTokens * wave;
-    Block cur[F::kSub];
+    // stage after stage into its slot; one without tokens counts as loaded all the same
+    const uint32_t stage0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)rows;
+    // keys and values of `valid` rows from slot t on
+    auto load_block = [&](int t, int page, int valid, int count, uint32_t to) {
+      const int64_t at = valid > 0 ? (int64_t)page * a.c.page_stride + (t & page_mask) * ts : 0;
 #pragma unroll
-    for (int s = 0; s < F::kSub; ++s) cur[s] = block_at(first + 16 * s);
-    uint32_t value[F::kRows][NV], value_e[F::kRows][NV];
-    auto load_values = [&](const Block* k) {
+      for (int s = 0; s < 2; ++s) {
+        const uint64_t base = (uint64_t)((s == 0 ? head_k : head_v) + at);
+        const v4i rsrc = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base),
+                          __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xFFFFu)),
+                          __builtin_amdgcn_readfirstlane(valid * ts), 0x00020000};
 #pragma unroll
-      for (int s = 0; s < F::kSub; ++s) {
-        const __amdgpu_buffer_rsrc_t r = rows_rsrc(a.c.v + k[s].base, k[s].valid * ts);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int v = 0; v < NV; ++v) {
-            if constexpr (EV == 8) value[4 * s + i][v] = __builtin_amdgcn_raw_buffer_load_b32(r, value_off[v] + i * ts, 0, kPolicy);
-            else value[4 * s + i][v] = __builtin_amdgcn_raw_buffer_load_b16(r, value_off[v] + i * ts, 0, kPolicy);
-            value_e[4 * s + i][v] = __builtin_amdgcn_raw_buffer_load_b8(r, value_scale[v] + i * ts, 0, kPolicy);
-          }
+        for (int j = 0; j < kMostLoads; ++j)
+          if (j < row_loads && 64 * j + lane < count * pieces) row_load<STREAM>(rsrc, to + s * F::kTokens * row_bytes + 1024 * j, row_off[j]);
       }
     };
-    load_keys(cur);
-    load_values(cur);
+    auto load_rows = [&](int t, const int* page, const int* valid, int slot) {
+      const uint32_t to = stage0 + slot * kStageBytes;
+      if (wide) {
+        load_block(t, page[0], valid[0] + valid[1], 32, to);
+      } else {
+        load_block(t, page[0], valid[0], 16, to);
+        load_block(t + 16, page[1], valid[1], 16, to + 16 * row_bytes);
+      }
+    };
+    auto landed_but_last = [&]() {
+      const int n = wide ? 2 * row_loads : 4 * row_loads;
+      if (n <= 2) landed<2>();
+      else if (n <= 4) landed<4>();
+      else if (n <= 6) landed<6>();
+      else if (n <= 8) landed<8>();
+      else if (n <= 10) landed<10>();
+      else landed<12>();
+    };
+    int page[F::kSub];                          // of the stage after those under way
+    int valid[F::kSub], valid_next[F::kSub];    // tokens of the current stage and the one after
+    auto pages_at = [&](int t) {
+      page[0] = page_at(t);
+      page[1] = wide ? page[0] : page_at(t + 16);
+    };
+    auto count_at = [&](int t, int* n) {
+      n[0] = valid_at(t, page[0], 16);
+      n[1] = valid_at(t + 16, page[1], 16);
+    };
+    pages_at(first);
+    count_at(first, valid);
+    // the queries are waited for here, so that turning them into operands does
+    // not wait for rows (loads are counted in order)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < KL; ++c)
+#pragma unroll
+        for (int l = 0; l < QL; ++l) asm volatile("" : "+v"(raw[nt][c][l]));
+    load_rows(first, page, valid, 0);
+    pages_at(first + kStep);
 
     // Queries, in parts: every wave reads them and writes a share.
 #pragma unroll
@@ -208,16 +259,25 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           constexpr int PER = 16 / (int)sizeof(X);
           const Chunk<X> v = __builtin_bit_cast(Chunk<X>, raw[nt][c][e / PER]);
           __bf16 part[PARTS];
-          split_query<PARTS>(in ? (float)v.e[e % PER] : 0.0f, part);
+          const float x = (float)v.e[e % PER];
+          split_query<PARTS>(in ? (a.scale_log2 < 0.0f ? -x : a.scale_log2 > 0.0f ? x : x * 0.0f) : 0.0f, part);
 #pragma unroll
           for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
         }
 #pragma unroll
-        for (int s = 0; s < PARTS; ++s) shared.in.query[nt][s][c][own_lane] = f[s];
+        for (int s = 0; s < PARTS; ++s) query[nt][s][c][own_lane] = f[s];
       }
     }
-    lds_barrier();                                // leaves keys and values under way
+    lds_barrier();                                // leaves rows under way
 
+    // the sign of the scale, or that it is 0, is in the queries
+    const float scale = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
+    constexpr bool kKeep = PARTS * KL * NT <= 4; // the queries' operands in registers
+    Frag kept[kKeep ? NT * PARTS * KL : 1];
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int i = 0; i < NT * PARTS * KL; ++i) kept[i] = (&query[0][0][0][0])[64 * i + lane];
+    }
     f32x4 acc[NT][NV][EV];
     float top[NT], base[NT], sum[NT];
 #pragma unroll
@@ -241,52 +301,90 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           const int hd = nt * kHeadTile + col;
           if (hd < held_heads)
             *(f32x4*)(scores + (int64_t)(held_from + k / F::kSub * kStep + k % F::kSub * 16) * group +
-                      16 * (tile0 * kHeadTile + hd)) = shared.in.held[wave][4 * held_heads * k + quad * held_heads + hd];
+                      16 * (tile0 * kHeadTile + hd)) = held[4 * held_heads * k + quad * held_heads + hd];
         }
       held_from += holding / F::kSub * kStep;
       holding = 0;
     };
 
-    for (int t = first; t < t1; t += kStep) {
+    auto step = [&](int t, auto slot_of) __attribute__((always_inline)) {
+      constexpr int kSlot = decltype(slot_of)::value;
       asm volatile("" ::: "memory");              // the queries stay in LDS
-      Block next[F::kSub];
+      const char* const stage = rows + kSlot * kStageBytes;
+      count_at(t + kStep, valid_next);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the slot held is read
+      load_rows(t + kStep, page, valid_next, 1 - kSlot);
+      pages_at(t + 2 * kStep);
+      landed_but_last();
+
+      uint32_t key[F::kSub][KL], key_e[F::kSub][(KL + 3) / 4], value[F::kRows][NV], value_e[F::kRows][NV];
 #pragma unroll
-      for (int s = 0; s < F::kSub; ++s) next[s] = block_at(t + kStep + 16 * s);
+      for (int s = 0; s < F::kSub; ++s) {
+        const char* row = stage + (16 * s + col) * row_bytes + quad * KL * 4;
+        const char* scales = stage + (16 * s + col) * row_bytes + D / 2 + quad * KL;
+#pragma unroll
+        for (int c = 0; c < KL; ++c) key[s][c] = ((const uint32_t*)row)[c];
+        if constexpr (KL == 2) {
+          key_e[s][0] = *(const uint16_t*)scales;
+        } else {
+#pragma unroll
+          for (int c = 0; c < KL / 4; ++c) key_e[s][c] = ((const uint32_t*)scales)[c];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < F::kRows; ++i) {
+        const char* row = stage + (F::kTokens + i / 4 * 16 + 4 * quad + i % 4) * row_bytes;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int d = (16 * v + col) * EV;
+          if constexpr (EV == 8) value[i][v] = *(const uint32_t*)(row + d / 2);
+          else value[i][v] = *(const uint16_t*)(row + d / 2);
+          value_e[i][v] = *(const uint8_t*)(row + D / 2 + d / 8);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);          // all asked for before the first is used
 
       Frag kf[F::kSub][KL];
 #pragma unroll
       for (int s = 0; s < F::kSub; ++s)
 #pragma unroll
         for (int c = 0; c < KL; ++c) {
-          const uint32_t e = key_e[s][c / 4] >> 8 * (c % 4) & 0xFFu & there[c];
+          const uint32_t e = key_e[s][c / 4];
+          const uint32_t at = c % 4 < 3 ? e << (23 - 8 * (c % 4)) : e >> 1;
           u32x4 w;
-          e2m1_decode(key[s][c] & there[c], e2m1_scale(e), (uint32_t*)&w);
+          e2m1_decode(key[s][c], __uint_as_float(at & (FULL ? 0x7F800000u : there[c])), (uint32_t*)&w);
           kf[s][c] = __builtin_bit_cast(Frag, w);
         }
-      load_keys(next);
 
-      float p[NT][F::kRows], tile_top[NT];
+      float dot[NT][F::kRows], tile_top[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        f32x4 dot[F::kSub];
+        f32x4 d[F::kSub];
 #pragma unroll
-        for (int s = 0; s < F::kSub; ++s) dot[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < F::kSub; ++s) d[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part)             // small terms first
 #pragma unroll
           for (int c = 0; c < KL; ++c) {
-            const Frag q = shared.in.query[nt][part][c][lane];
+            const Frag q = kKeep ? kept[kKeep ? (nt * PARTS + part) * KL + c : 0] : query[nt][part][c][lane];
 #pragma unroll
-            for (int s = 0; s < F::kSub; ++s) dot[s] = mul(kf[s][c], q, dot[s]);
+            for (int s = 0; s < F::kSub; ++s) d[s] = mul(kf[s][c], q, d[s]);
           }
-        tile_top[nt] = -INFINITY;
 #pragma unroll
-        for (int s = 0; s < F::kSub; ++s)
+        for (int i = 0; i < F::kRows; ++i) dot[nt][i] = d[i / 4][i % 4];
+      }
+      if (valid[0] + valid[1] < F::kTokens) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[nt][4 * s + i] = 4 * quad + i < cur[s].valid ? dot[s][i] * a.scale_log2 : -INFINITY;
-            tile_top[nt] = fmaxf(tile_top[nt], p[nt][4 * s + i]);
-          }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < F::kRows; ++i) dot[nt][i] = 4 * quad + i % 4 < valid[i / 4] ? dot[nt][i] : -INFINITY;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        tile_top[nt] = dot[nt][0];
+#pragma unroll
+        for (int i = 1; i < F::kRows; ++i) tile_top[nt] = fmaxf(tile_top[nt], dot[nt][i]);
+        tile_top[nt] *= scale;
       }
       if (a.accumulate) {
         if (4 * held_heads * (holding + F::kSub) > kHold) release();
@@ -296,13 +394,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           for (int s = 0; s < F::kSub; ++s) {
             const int hd = nt * kHeadTile + col;
             if (hd < held_heads)
-              shared.in.held[wave][4 * held_heads * (holding + s) + quad * held_heads + hd] =
-                  f32x4{p[nt][4 * s], p[nt][4 * s + 1], p[nt][4 * s + 2], p[nt][4 * s + 3]};
+              held[4 * held_heads * (holding + s) + quad * held_heads + hd] =
+                  f32x4{dot[nt][4 * s], dot[nt][4 * s + 1], dot[nt][4 * s + 2], dot[nt][4 * s + 3]} * scale;
           }
         holding += F::kSub;
       }
 
-      Frag pf[NT][WPARTS];
+      u32x4 pf[NT][WPARTS];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
@@ -318,13 +416,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           base[nt] = rescaled;
         }
 #pragma unroll
-        for (int i = 0; i < F::kRows; ++i) {
-          const float w = exp2_fast(p[nt][i] - base[nt]);
-          sum[nt] += w;
-          __bf16 part[WPARTS];
-          split<__bf16, WPARTS>(w, part);
+        for (int i = 0; i < F::kRows; i += 2) {
+          const float w0 = exp2_fast(fmaf(dot[nt][i], scale, -base[nt])), w1 = exp2_fast(fmaf(dot[nt][i + 1], scale, -base[nt]));
+          sum[nt] += w0 + w1;
+          uint32_t part[WPARTS];
+          split_pair<WPARTS>(w0, w1, part);
 #pragma unroll
-          for (int s = 0; s < WPARTS; ++s) pf[nt][s][i] = part[s];
+          for (int s = 0; s < WPARTS; ++s) pf[nt][s][i / 2] = part[s];
         }
       }
 
@@ -342,22 +440,33 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           }
         }
 #pragma unroll
-        for (int j = 0; j < EV; ++j) {
-          u32x4 w;                                  // tokens of a column
+        for (int j = 0; j < EV; j += 2) {
+          u32x4 w[2];                               // tokens of two columns
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = __builtin_amdgcn_perm(x[2 * i + 1][j / 2], x[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-          const Frag vf = __builtin_bit_cast(Frag, w);
+          for (int i = 0; i < 4; ++i) {
+            w[0][i] = __builtin_amdgcn_perm(x[2 * i + 1][j / 2], x[2 * i][j / 2], 0x05040100u);
+            w[1][i] = __builtin_amdgcn_perm(x[2 * i + 1][j / 2], x[2 * i][j / 2], 0x07060302u);
+          }
 #pragma unroll
           for (int part = WPARTS - 1; part >= 0; --part)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][v][j] = mul(vf, pf[nt][part], acc[nt][v][j]);
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int o = 0; o < 2; ++o)
+                acc[nt][v][j + o] = mul(__builtin_bit_cast(Frag, w[o]), __builtin_bit_cast(Frag, pf[nt][part]), acc[nt][v][j + o]);
         }
       }
 #pragma unroll
-      for (int s = 0; s < F::kSub; ++s) cur[s] = next[s];
-      load_values(cur);
+      for (int s = 0; s < F::kSub; ++s) {
+        valid[s] = valid_next[s];
+      }
+    };
+    for (int t = first; t < t1; t += 2 * kStep) {
+      step(t, std::integral_constant<int, 0>());
+      if (t + kStep >= t1) break;
+      step(t + kStep, std::integral_constant<int, 1>());
     }
+    landed<0>();                                  // the outputs come where rows were
     if (a.accumulate) release();
 
     // join the waves
@@ -387,7 +496,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < EV; j += 4)
-              *(f32x4*)&shared.slab[wave][own_col][(16 * v + 4 * own_quad + i) * EV + j] =
+              *(f32x4*)&slab[wave][own_col][(16 * v + 4 * own_quad + i) * EV + j] =
                   f32x4{acc[nt][v][j][i], acc[nt][v][j + 1][i], acc[nt][v][j + 2][i], acc[nt][v][j + 3][i]} * f;
       }
       __syncthreads();
@@ -398,7 +507,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
         float common = -INFINITY, weight = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          o += *(const f32x4*)&shared.slab[w][hd][4 * c];
+          o += *(const f32x4*)&slab[w][hd][4 * c];
           common = fmaxf(common, stat[nt][w][hd][0]);
         }
 #pragma unroll
@@ -425,30 +534,39 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
   }
 }
 
-template <int XT, int DP>
-void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
+template <int XT, int DP, int NT, bool FULL, bool STREAM>
+void launch_kernel(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
   const int64_t shares = (int64_t)a.c.kv_heads * p.workgroups;
   const dim3 grid(kXcds * p.tile_groups, (unsigned)((shares + kXcds - 1) / kXcds)), block(64 * kWaves);
+  const int bytes = Lds<XT, DP, NT>::bytes(a.accumulate);
+  cache_attend_e2m1_kernel<XT, DP, NT, FULL, STREAM><<<grid, block, bytes, s>>>(a, w, p.workgroups);
+}
+
+template <int XT, int DP, bool FULL>
+void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
   if constexpr (DP < 256) {
-    if (p.wave_tiles == 2) {
-      if (p.tile_groups == 1) cache_attend_e2m1_kernel<XT, DP, 2, true><<<grid, block, 0, s>>>(a, w, p.workgroups);
-      else cache_attend_e2m1_kernel<XT, DP, 2, false><<<grid, block, 0, s>>>(a, w, p.workgroups);
-      return;
-    }
-  } else if (p.tile_groups > 1) {
-    cache_attend_e2m1_kernel<XT, DP, 1, false><<<grid, block, 0, s>>>(a, w, p.workgroups);
-    return;
+    if (p.wave_tiles == 1) launch_kernel<XT, DP, 1, FULL, true>(a, w, p, s);
+    else if (p.tile_groups == 1) launch_kernel<XT, DP, 2, FULL, true>(a, w, p, s);
+    else launch_kernel<XT, DP, 2, FULL, false>(a, w, p, s);
+  } else {
+    if (p.tile_groups == 1) launch_kernel<XT, DP, 1, FULL, true>(a, w, p, s);
+    else launch_kernel<XT, DP, 1, FULL, false>(a, w, p, s);
   }
-  cache_attend_e2m1_kernel<XT, DP, 1, true><<<grid, block, 0, s>>>(a, w, p.workgroups);
+}
+
+template <int XT, int DP>
+void launch_dim(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
+  if (a.c.head_dim == DP) launch_tiles<XT, DP, true>(a, w, p, s);
+  else launch_tiles<XT, DP, false>(a, w, p, s);
 }
 
 template <int XT>
 hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
   const Plan p = plan_of(a.c, a.heads, a.max_len);
   const Work w = work_of(a, p);
-  if (a.c.head_dim <= 64) launch_tiles<XT, 64>(a, w, p, s);
-  else if (a.c.head_dim <= 128) launch_tiles<XT, 128>(a, w, p, s);
-  else launch_tiles<XT, 256>(a, w, p, s);
+  if (a.c.head_dim <= 64) launch_dim<XT, 64>(a, w, p, s);
+  else if (a.c.head_dim <= 128) launch_dim<XT, 128>(a, w, p, s);
+  else launch_dim<XT, 256>(a, w, p, s);
   launch_join<XT>(a, w, p, s);
   return hipGetLastError();
 }

@@ -156,6 +156,16 @@ def test_scales_far_from_one(act, spread):
 
 
 @pytest.mark.parametrize("act", eu.ACTS)
+@pytest.mark.parametrize("scale", (0.0, -0.2, 1.5))
+def test_scale(act, scale):
+    """Zero weighs all tokens alike, a negative one turns the scores round."""
+    c = eu.make_cache((77, 1, 0, 300), 2, 64, 16, 43, evicts=True)
+    before = [eu.get(c, "weights", b, n) for b, n in enumerate((77, 1, 0, 300))]
+    q, out, _ = run(c, 4, act, 44, accumulate=True, scale=scale)
+    check(c, q, 4, out, act, scale, before)
+
+
+@pytest.mark.parametrize("act", eu.ACTS)
 def test_max_len_and_lengths_out_of_range(act):
     c = eu.make_cache((200, 33, 64, 64), 2, 64, 32, 35)
     q, out, scale = run(c, 4, act, 36, max_len=50)
