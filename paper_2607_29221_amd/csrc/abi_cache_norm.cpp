@@ -21,7 +21,7 @@ mosaic_status mosaic_cache_read(const mosaic_kv_cache* cache, const int32_t* len
   mosaic_status st = view_of(cache, &a.c);
   if (st != MOSAIC_OK) return st;
   if (rows < 0) return fail(MOSAIC_ERR_INVALID_ARG, "negative size");
-  if (rows > kMaxSlots) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^30 rows");
+  if (rows > (1 << 24)) return fail(MOSAIC_ERR_UNSUPPORTED, "more than 2^24 rows");
   if (starts == nullptr && rows != a.c.batch)
     return fail(MOSAIC_ERR_INVALID_ARG, "%lld rows for %d sequences need starts", (long long)rows, a.c.batch);
   if (a.c.batch == 0 && rows > 0) return fail(MOSAIC_ERR_INVALID_ARG, "tokens of no sequence");
