@@ -102,8 +102,11 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // where the registers hold one, 178 and 180 us). Never more than fit at
   // once, since a unit with two takes twice as long (12 key/value heads: 249 us
   // with 264, 173 us with 252), but more per unit where more than one unit in 16
-  // would idle (71 heads: 217 us with 213, 186 us with 497).
-  int32_t slots = c.dtype == MOSAIC_E2M1 ? 512 : p.tile_groups > 1 && c.head_dim <= 128 ? 512 : 256;
+  // would idle (71 heads: 217 us with 213, 186 us with 497). Over 4 bits, where the
+  // arithmetic takes as long as the rows, two per unit as long as its LDS holds them
+  // (131072 tokens of 32 and 8 heads: 39 us with 256 in all, 35 with 512, 37.5 with 768).
+  const bool two = c.head_dim <= 128 && (p.tile_groups > 1 || c.dtype == MOSAIC_E2M1);
+  int32_t slots = two ? 512 : 256;
   int64_t wanted;
   while (true) {
     const int64_t shares = p.tile_groups > 1 ? slots / kXcds / p.tile_groups * kXcds : slots;
@@ -127,28 +130,49 @@ int64_t part_floats(const CacheView& c, int32_t heads, const Plan& p) {
   return ((int64_t)c.batch + p.workgroups) * heads * c.head_dim;
 }
 
+// Over 4 bits a sequence counts kStartSteps more steps behind its own: to begin
+// another one costs a workgroup about as long (64 sequences of 512 to 7168 tokens:
+// without, a workgroup's end lay between 45 and 70 us). Where shares are shorter
+// than kLongShare steps it would leave workgroups without any.
+constexpr int kStartSteps = 2, kLongShare = 16;
+
 // Steps of sequence i, 0 beyond the batch.
-__device__ __forceinline__ int steps_of(const AttendLaunch& a, int i) {
-  return i < a.c.batch ? (held_tokens(a.lengths, i, a.max_len) + kStepTokens - 1) / kStepTokens : 0;
+__device__ __forceinline__ int steps_of(const AttendLaunch& a, int i, int extra) {
+  const int steps = i < a.c.batch ? (held_tokens(a.lengths, i, a.max_len) + kStepTokens - 1) / kStepTokens : 0;
+  return steps > 0 ? steps + extra : 0;
 }
-// Steps of the first 64 sequences, a lane each: its own, and all up to it.
+// Steps of the first 64 sequences, a lane each: its own, and all up to it; and
+// what all sequences count more.
 struct FirstSteps {
-  int own, upto;
+  int own, upto, extra;
 };
 // Steps of all sequences, by one wave.
 __device__ __forceinline__ int all_steps(const AttendLaunch& a, int lane, FirstSteps* first) {
-  first->own = steps_of(a, lane);
+  first->own = steps_of(a, lane, first->extra);
   first->upto = wave_scan(first->own);
   int total = __builtin_amdgcn_readlane(first->upto, 63);
-  for (int i0 = 64; i0 < a.c.batch; i0 += 64) total += __builtin_amdgcn_readlane(wave_scan(steps_of(a, i0 + lane)), 63);
+  for (int i0 = 64; i0 < a.c.batch; i0 += 64)
+    total += __builtin_amdgcn_readlane(wave_scan(steps_of(a, i0 + lane, first->extra)), 63);
   return total;
+}
+// Steps of a share, at least 1, and in *total those of all sequences. starts:
+// whether sequences may count more than their own.
+__device__ __forceinline__ int share_of_steps(const AttendLaunch& a, int lane, int workgroups, bool starts, FirstSteps* first,
+                                              int* total) {
+  first->extra = 0;
+  *total = all_steps(a, lane, first);
+  if (starts && a.c.batch > 1 && *total / workgroups >= kLongShare) {
+    first->extra = kStartSteps;
+    *total = all_steps(a, lane, first);
+  }
+  return max((*total + workgroups - 1) / workgroups, 1);
 }
 // Steps of the sequences before b.
 __device__ __forceinline__ int steps_before(const AttendLaunch& a, int lane, int b, const FirstSteps& first) {
   if (b < 64) return __builtin_amdgcn_readlane(first.upto - first.own, b);
   int carry = __builtin_amdgcn_readlane(first.upto, 63);
   for (int i0 = 64; ; i0 += 64) {
-    const int own = steps_of(a, i0 + lane), upto = wave_scan(own);
+    const int own = steps_of(a, i0 + lane, first.extra), upto = wave_scan(own);
     if (b < i0 + 64) return carry + __builtin_amdgcn_readlane(upto - own, b - i0);
     carry += __builtin_amdgcn_readlane(upto, 63);
   }
@@ -167,10 +191,11 @@ __device__ __forceinline__ int sequence_at(const AttendLaunch& a, int lane, int 
     i0 += 64;
     if (i0 >= a.c.batch) return -1;
     carry += __builtin_amdgcn_readlane(upto, 63);
-    own = steps_of(a, i0 + lane);
+    own = steps_of(a, i0 + lane, first.extra);
     upto = wave_scan(own);
   }
 }
+
 // Base and sum of a head over its parts, `stride` floats apart, by one wave.
 __device__ __forceinline__ void head_norm(const float* st, int64_t stride, int parts, int lane, float* common,
                                           float* sum) {
@@ -204,7 +229,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendLaunch a, Work wk
   const int out_groups = (group + out_heads - 1) / out_heads;
   const int n = held_tokens_uniform(a.lengths, b, a.max_len);
   FirstSteps first64;
-  const int total = all_steps(a, lane, &first64), share = max((total + workgroups - 1) / workgroups, 1);
+  int total;
+  const int share = share_of_steps(a, lane, workgroups, a.c.dtype == MOSAIC_E2M1, &first64, &total);
   const int before = steps_before(a, lane, b, first64);
   const int steps = (n + kStepTokens - 1) / kStepTokens, u0 = before / share;
   const int parts = steps == 0 ? 0 : (before + steps - 1) / share - u0 + 1;

@@ -142,9 +142,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_ke
   if (u >= workgroups) return;
   const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
 
-  int before;
+  int before, total;
   FirstSteps first64;
-  const int total = all_steps(a, lane, &first64), share = (total + workgroups - 1) / workgroups;
+  const int share = share_of_steps(a, lane, workgroups, false, &first64, &total);
   int at = u * share;
   const int stop = min(total, at + share);
   if (at >= stop) return;

@@ -10,12 +10,26 @@
 // bits), one of a bf16 one, two of a weight for 16-bit outputs (at most 2^-17
 // of it is left out, where the output's rounding takes 2^-12 or more).
 //
+// * Rows of 80 bytes (of 128 elements) make small pieces of codes and scales. They
+//   come to LDS whole, 16 bytes per lane, past the caches: read piece by piece from
+//   memory, the same lines were asked for several times (131072 tokens 45 us, 40 us
+//   through the caches, 35 us by way of LDS). A wave has two stages of 32 tokens
+//   and waits for its own loads only.
 // * Keys: the 16 lanes of a quarter take one token each, a quarter of its row:
 //   dwords of codes and as many scale bytes lie side by side. The inner
 //   dimension's order differs from the elements' by that, in the queries too.
 // * Values: a lane takes the same 8 columns (4 where head_dim is at most 64) of
 //   8 tokens, a dword of codes and a scale byte each, and turns them with byte
 //   permutes once they are bf16.
+//
+// Measured on an MI355X with the join, heads of 128 elements: 131072 tokens of one
+// sequence, 32 query and 8 key/value heads, bf16, 35 us, 27 to 31 us in this kernel
+// (168 MB: 5.4 to 6.2 TB/s); 64 sequences of 512 to 7168 tokens, 64 and 8 heads,
+// bf16 62 us, float32 71 to 75 us (315 MB: 5.8 and 4.9 TB/s in this kernel). What is
+// left above the bandwidth: with the loads alone the 64 sequences take 61 us, with
+// the arithmetic alone 65 (before parts lay side by side); a part of a sequence
+// starts with 3.5 to 5.5 us of dependent loads, and about 200 vector instructions
+// per 32 tokens and wave leave the two waves of a SIMD little room.
 #include <cfloat>
 #include <type_traits>
 
@@ -89,14 +103,21 @@ template <int PARTS> __device__ __forceinline__ void split_pair(float x, float y
   }
 }
 
+// The value N columns further on, of 16 that come round.
+template <int N> __device__ __forceinline__ float other_column(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + N, 0xF, 0xF, true));
+}
+
 // Bytes of LDS: operands of the first product by lane; the waves' stages of rows;
 // where weights are added up, scores on their way to memory. The waves' outputs
 // come over these at the end.
-template <int XT, int DP, int NT> struct Lds {
+template <int XT, int DP, int NT, int W> struct Lds {
   typedef Form<XT, DP> F;
+  static constexpr int kSlots = kHeadTile / W;  // parts of a head, side by side
+  static constexpr int kPasses = (F::kParts + kSlots - 1) / kSlots, kWeightPasses = (F::kWeightParts + kSlots - 1) / kSlots;
   static constexpr int kStages = 2;             // of a wave, kTokens rows of keys and of values each
   static constexpr int kStageBytes = 2 * F::kTokens * MOSAIC_E2M1_ROW_BYTES(DP);
-  static constexpr int kQuery = NT * F::kParts * F::kKeyDwords * 64 * 16;
+  static constexpr int kQuery = NT * kPasses * F::kKeyDwords * 64 * 16;
   static constexpr int kRows = kWaves * kStages * kStageBytes;
   static constexpr int kPast = 256;             // columns past head_dim are read from what follows a row
   static constexpr int kHold = 128 * NT;        // of a wave's scores, 16 bytes each: one step's at least
@@ -107,23 +128,27 @@ template <int XT, int DP, int NT> struct Lds {
   }
 };
 
-// NT: blocks of 16 query heads per wave. FULL: head_dim is DP. STREAM: past the
-// caches, as no other workgroup reads the same rows.
-template <int XT, int DP, int NT, bool FULL, bool STREAM>
+// NT: blocks of 16 query heads per wave. W: where a group has at most 8 or 4
+// heads, columns W, 2W, ... of a block hold further parts of the heads in the first
+// W, so that a product takes several parts at a time (64 sequences, 64 query and 8
+// key/value heads, float32: 73.4 us without, 70.7 us with). FULL: head_dim is DP.
+// STREAM: past the caches, as no other workgroup reads the same rows.
+template <int XT, int DP, int NT, int W, bool FULL, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2m1_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef Form<XT, DP> F;
-  typedef Lds<XT, DP, NT> S;
+  typedef Lds<XT, DP, NT, W> S;
   typedef typename F::X X;
   typedef bf16x8 Frag;
   constexpr int KL = F::kKeyDwords, NV = F::kValuePieces, EV = F::kEach, PARTS = F::kParts, WPARTS = F::kWeightParts;
+  constexpr int R = S::kSlots, PASSES = S::kPasses, WPASSES = S::kWeightPasses;
   constexpr int kHold = S::kHold, kStages = S::kStages, kStageBytes = S::kStageBytes;
   constexpr int kMostLoads = (2 * MOSAIC_E2M1_ROW_BYTES(DP) / 16 + 3) / 4;   // per 32 rows
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float stat[NT][kWaves][kHeadTile][2];
-  Frag(*query)[PARTS][KL][64] = (Frag(*)[PARTS][KL][64])lds;
+  Frag(*query)[PASSES][KL][64] = (Frag(*)[PASSES][KL][64])lds;
   float(*slab)[kHeadTile][DP + 4] = (float(*)[kHeadTile][DP + 4])lds;
 
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4, slot_of_col = col / W;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const char* const rows = lds + S::kQuery + wave * kStages * kStageBytes;
   f32x4* const held = (f32x4*)(lds + S::kQuery + S::kRows + S::kPast) + wave * kHold;
@@ -133,9 +158,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
   if (u >= workgroups) return;
   const int group = a.heads / a.c.kv_heads, D = FULL ? DP : a.c.head_dim;
 
-  int before;
+  int before, total;
   FirstSteps first64;
-  const int total = all_steps(a, lane, &first64), share = (total + workgroups - 1) / workgroups;
+  const int share = share_of_steps(a, lane, workgroups, true, &first64, &total);
   int at = u * share;
   const int stop = min(total, at + share);
   if (at >= stop) return;
@@ -143,6 +168,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
   if (b < 0) return;
   while (true) {
     const int n = held_tokens_uniform(a.lengths, b, a.max_len), steps = (n + kStepTokens - 1) / kStepTokens;
+    if (at - before >= steps) {                   // the share begins behind the sequence's own steps: nothing of it
+      at = before + steps + first64.extra;
+      if (at >= stop) return;
+      before = at;
+      do {
+        if (++b >= a.c.batch) return;
+      } while (held_tokens_uniform(a.lengths, b, a.max_len) == 0);
+      continue;
+    }
     const int t0 = (at - before) * kStepTokens, t1 = min(n, min(stop - before, steps) * kStepTokens);
 
     // What only the start and the end of a part need is computed there.
@@ -155,7 +189,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     u32x4 raw[NT][KL][QL];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int head = min((tile0 + nt) * kHeadTile + (own_lane & 15), group - 1);
+      const int head = min((tile0 + nt) * kHeadTile + (own_lane & (W - 1)), group - 1);
       const char* row = (const char*)a.q + (int64_t)b * a.ldq + ((int64_t)h * group + head) * D * (int)sizeof(X);
 #pragma unroll
       for (int c = 0; c < KL; ++c)
@@ -248,12 +282,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     // Queries, in parts: every wave reads them and writes a share.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int head = (tile0 + nt) * kHeadTile + (own_lane & 15);
+      const int head = (tile0 + nt) * kHeadTile + (own_lane & (W - 1)), part0 = (own_lane & 15) / W;
 #pragma unroll
       for (int c = 0; c < KL; ++c) {
         if (c % kWaves != wave) continue;
         const bool in = head < group && ((own_lane >> 4) * KL + c) * 8 < D;
-        Frag f[PARTS];
+        Frag f[PASSES];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           constexpr int PER = 16 / (int)sizeof(X);
@@ -262,24 +296,30 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           const float x = (float)v.e[e % PER];
           split_query<PARTS>(in ? (a.scale_log2 < 0.0f ? -x : a.scale_log2 > 0.0f ? x : x * 0.0f) : 0.0f, part);
 #pragma unroll
-          for (int s = 0; s < PARTS; ++s) f[s][e] = part[s];
+          for (int s = 0; s < PASSES; ++s) {
+            f[s][e] = PARTS == 1 ? part[0] : (__bf16)0.0f;       // one part: the same in all columns of a head
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+              if (PARTS > 1 && s * R + part0 == i) f[s][e] = part[i];
+          }
         }
 #pragma unroll
-        for (int s = 0; s < PARTS; ++s) query[nt][s][c][own_lane] = f[s];
+        for (int s = 0; s < PASSES; ++s) query[nt][s][c][own_lane] = f[s];
       }
     }
     lds_barrier();                                // leaves rows under way
 
     // the sign of the scale, or that it is 0, is in the queries
     const float scale = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
-    constexpr bool kKeep = PARTS * KL * NT <= 4; // the queries' operands in registers
-    Frag kept[kKeep ? NT * PARTS * KL : 1];
+    constexpr bool kKeep = PASSES * KL * NT <= 4; // the queries' operands in registers
+    Frag kept[kKeep ? NT * PASSES * KL : 1];
     if constexpr (kKeep) {
 #pragma unroll
-      for (int i = 0; i < NT * PARTS * KL; ++i) kept[i] = (&query[0][0][0][0])[64 * i + lane];
+      for (int i = 0; i < NT * PASSES * KL; ++i) kept[i] = (&query[0][0][0][0])[64 * i + lane];
     }
     f32x4 acc[NT][NV][EV];
-    float top[NT], base[NT], sum[NT];
+    float top[NT], base[NT];
+    f32x4 sum[NT];                              // of the weights: their products with ones
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -287,7 +327,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
 #pragma unroll
         for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       top[nt] = -INFINITY;
-      base[nt] = sum[nt] = 0.0f;
+      base[nt] = 0.0f;
+      sum[nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
     // Scores go to memory through LDS, many steps at a time.
@@ -310,6 +351,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     auto step = [&](int t, auto slot_of) __attribute__((always_inline)) {
       constexpr int kSlot = decltype(slot_of)::value;
       asm volatile("" ::: "memory");              // the queries stay in LDS
+      // Of two waves on a SIMD the older one goes first and would end long before the
+      // other: raised in every second step, neither runs ahead (64 sequences 75.0 and
+      // 74.5 us, one of 65536 tokens 26.4 and 25.2 us).
+      __builtin_amdgcn_s_setprio(kSlot == 0 ? 2 : 0);
       const char* const stage = rows + kSlot * kStageBytes;
       count_at(t + kStep, valid_next);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the slot held is read
@@ -352,7 +397,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
           const uint32_t e = key_e[s][c / 4];
           const uint32_t at = c % 4 < 3 ? e << (23 - 8 * (c % 4)) : e >> 1;
           u32x4 w;
-          e2m1_decode(key[s][c], __uint_as_float(at & (FULL ? 0x7F800000u : there[c])), (uint32_t*)&w);
+          e2m1_decode(key[s][c], __uint_as_float(FULL ? at : at & there[c]), (uint32_t*)&w);   // of a scale, the exponent counts
           kf[s][c] = __builtin_bit_cast(Frag, w);
         }
 
@@ -363,15 +408,20 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
 #pragma unroll
         for (int s = 0; s < F::kSub; ++s) d[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part)             // small terms first
+        for (int part = PASSES - 1; part >= 0; --part)            // small terms first
 #pragma unroll
           for (int c = 0; c < KL; ++c) {
-            const Frag q = kKeep ? kept[kKeep ? (nt * PARTS + part) * KL + c : 0] : query[nt][part][c][lane];
+            const Frag q = kKeep ? kept[kKeep ? (nt * PASSES + part) * KL + c : 0] : query[nt][part][c][lane];
 #pragma unroll
             for (int s = 0; s < F::kSub; ++s) d[s] = mul(kf[s][c], q, d[s]);
           }
 #pragma unroll
-        for (int i = 0; i < F::kRows; ++i) dot[nt][i] = d[i / 4][i % 4];
+        for (int i = 0; i < F::kRows; ++i) {
+          float x = d[i / 4][i % 4];
+          if (PARTS > 1 && R > 1) x += other_column<8>(x);       // the parts' scores: the same sum in all columns
+          if (PARTS > 1 && R > 2) x += other_column<4>(x);
+          dot[nt][i] = x;
+        }
       }
       if (valid[0] + valid[1] < F::kTokens) {
 #pragma unroll
@@ -400,7 +450,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
         holding += F::kSub;
       }
 
-      u32x4 pf[NT][WPARTS];
+      u32x4 pf[NT][WPASSES];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (__any(tile_top[nt] > top[nt] + F::kSlack)) {
@@ -418,14 +468,24 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
 #pragma unroll
         for (int i = 0; i < F::kRows; i += 2) {
           const float w0 = exp2_fast(fmaf(dot[nt][i], scale, -base[nt])), w1 = exp2_fast(fmaf(dot[nt][i + 1], scale, -base[nt]));
-          sum[nt] += w0 + w1;
           uint32_t part[WPARTS];
           split_pair<WPARTS>(w0, w1, part);
 #pragma unroll
-          for (int s = 0; s < WPARTS; ++s) pf[nt][s][i / 2] = part[s];
+          for (int s = 0; s < WPASSES; ++s) {
+            pf[nt][s][i / 2] = s * R < WPARTS ? part[s * R] : 0u;
+#pragma unroll
+            for (int o = 1; o < R; ++o)
+              if (slot_of_col == o) pf[nt][s][i / 2] = s * R + o < WPARTS ? part[s * R + o < WPARTS ? s * R + o : 0] : 0u;
+          }
         }
       }
 
+      const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+      for (int part = WPASSES - 1; part >= 0; --part)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          sum[nt] = mul(__builtin_bit_cast(Frag, ones), __builtin_bit_cast(Frag, pf[nt][part]), sum[nt]);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         uint32_t x[F::kRows][EV / 2];               // pairs of a token's columns
@@ -448,7 +508,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
             w[1][i] = __builtin_amdgcn_perm(x[2 * i + 1][j / 2], x[2 * i][j / 2], 0x07060302u);
           }
 #pragma unroll
-          for (int part = WPARTS - 1; part >= 0; --part)
+          for (int part = WPASSES - 1; part >= 0; --part)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -474,7 +534,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     const int own_col = own_lane & 15, own_quad = own_lane >> 4;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const float all = head_sum(sum[nt]);
+      float all = sum[nt][0];                     // of this column's parts: the same in all rows
+      if (R > 1) all += other_column<8>(all);
+      if (R > 2) all += other_column<4>(all);
       if (own_quad == 0) {
         stat[nt][wave][own_col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
         stat[nt][wave][own_col][1] = all;
@@ -507,7 +569,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
         float common = -INFINITY, weight = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          o += *(const f32x4*)&slab[w][hd][4 * c];
+#pragma unroll
+          for (int i = (R < WPARTS ? R : WPARTS) - 1; i >= 0; --i) o += *(const f32x4*)&slab[w][hd + i * W][4 * c];
           common = fmaxf(common, stat[nt][w][hd][0]);
         }
 #pragma unroll
@@ -524,7 +587,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     }
 
     // on to the next sequence of this share
-    at = before + steps;
+    at = before + steps + first64.extra;
     if (at >= stop) return;
     __syncthreads();                              // the outputs are read
     before = at;
@@ -534,23 +597,28 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
   }
 }
 
-template <int XT, int DP, int NT, bool FULL, bool STREAM>
+template <int XT, int DP, int NT, int W, bool FULL, bool STREAM>
 void launch_kernel(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
   const int64_t shares = (int64_t)a.c.kv_heads * p.workgroups;
   const dim3 grid(kXcds * p.tile_groups, (unsigned)((shares + kXcds - 1) / kXcds)), block(64 * kWaves);
-  const int bytes = Lds<XT, DP, NT>::bytes(a.accumulate);
-  cache_attend_e2m1_kernel<XT, DP, NT, FULL, STREAM><<<grid, block, bytes, s>>>(a, w, p.workgroups);
+  const int bytes = Lds<XT, DP, NT, W>::bytes(a.accumulate);
+  cache_attend_e2m1_kernel<XT, DP, NT, W, FULL, STREAM><<<grid, block, bytes, s>>>(a, w, p.workgroups);
 }
 
 template <int XT, int DP, bool FULL>
 void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
+  const int32_t group = a.heads / a.c.kv_heads;
+  if constexpr (FULL) {
+    if (group <= 4) return launch_kernel<XT, DP, 1, 4, FULL, true>(a, w, p, s);
+    if (group <= 8) return launch_kernel<XT, DP, 1, 8, FULL, true>(a, w, p, s);
+  }
   if constexpr (DP < 256) {
-    if (p.wave_tiles == 1) launch_kernel<XT, DP, 1, FULL, true>(a, w, p, s);
-    else if (p.tile_groups == 1) launch_kernel<XT, DP, 2, FULL, true>(a, w, p, s);
-    else launch_kernel<XT, DP, 2, FULL, false>(a, w, p, s);
+    if (p.wave_tiles == 1) launch_kernel<XT, DP, 1, 16, FULL, true>(a, w, p, s);
+    else if (p.tile_groups == 1) launch_kernel<XT, DP, 2, 16, FULL, true>(a, w, p, s);
+    else launch_kernel<XT, DP, 2, 16, FULL, false>(a, w, p, s);
   } else {
-    if (p.tile_groups == 1) launch_kernel<XT, DP, 1, FULL, true>(a, w, p, s);
-    else launch_kernel<XT, DP, 1, FULL, false>(a, w, p, s);
+    if (p.tile_groups == 1) launch_kernel<XT, DP, 1, 16, FULL, true>(a, w, p, s);
+    else launch_kernel<XT, DP, 1, 16, FULL, false>(a, w, p, s);
   }
 }
 
