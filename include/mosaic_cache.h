@@ -146,7 +146,8 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
  * float64 and rounded to a float32 factor; from there on each product and sum
  * of the element and of its rotation is rounded to float32 by itself (nothing
  * is fused), here and wherever the cache is in 4 bits: a key between two codes
- * takes the same one in any computation of these formulas. eps >= 0, finite. */
+ * takes the same one in any computation of these formulas. eps >= 0, finite; the
+ * weights lie in none of the outputs. */
 typedef struct mosaic_qk_norm {
   const float* q_weight;      /* head_dim entries each, 4-byte aligned */
   const float* k_weight;
@@ -157,7 +158,7 @@ mosaic_status mosaic_cache_append_norm(const mosaic_kv_cache* cache, const void*
                                        const mosaic_rotary* rotary, void* q_out, int64_t ldq, const int32_t* state,
                                        int32_t* new_state, void* stream);
 
-/* Cached tokens as rows: row t of k_out and v_out (rows x kv_heads * head_dim
+/* Cached tokens as rows, at most 2^24: row t of k_out and v_out (rows x kv_heads * head_dim
  * of out_dtype, MOSAIC_F32 or the cache's type, any of the three over 4 bits)
  * gets the keys and values of slot first[b] + (t - starts[b]) of the sequence
  * b with starts[b] <= t < starts[b + 1] (starts as above; NULL: row b is

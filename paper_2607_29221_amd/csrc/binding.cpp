@@ -165,9 +165,10 @@ class Rng {
   bool held_ = false;
 };
 
-// The current stream of the current device.
-bool current_stream(void** s) {
+// The current stream of the current device (and which one it is).
+bool current_stream(void** s, int64_t* device = nullptr) {
   PyObject* d = PyObject_CallNoArgs(get_device);
+  if (d != nullptr && device != nullptr) *device = PyLong_AsLongLong(d);
   PyObject* r = d != nullptr ? PyObject_CallOneArg(get_stream, d) : nullptr;
   Py_XDECREF(d);
   if (r == nullptr) {
@@ -561,6 +562,8 @@ struct Cache {
     c.token_stride = k->stride(2);
     c.ldt = t->size(0) > 1 ? t->stride(0) : t->size(1);   // a single row's stride has no meaning
     if (!state_like(st) || (w != nullptr && !numbers(w, at::kFloat)) || (r != nullptr && !numbers(r, at::kInt))) return false;
+    for (const at::Tensor* x : {v, t, st, w, r})
+      if (x != nullptr && x->device() != k->device()) return false;
     c.k = k->data_ptr();
     c.v = v->data_ptr();
     c.block_table = (const int32_t*)t->data_ptr();
@@ -577,8 +580,13 @@ struct Cache {
     const at::Tensor* t = plain(o);
     if (t == nullptr || (t->scalar_type() != at::kFloat && t->scalar_type() != dtype && !four)) return false;
     *type = ftype(t->scalar_type());
-    if (*type < 0) return false;
+    if (*type < 0 || t->device() != device) return false;
     return matrix(o, n, cols, t->scalar_type(), false, m);
+  }
+  // the current stream, of the device that the cache is on
+  bool stream(void** s) const {
+    int64_t current = -1;
+    return current_stream(s, &current) && current == device.index();
   }
   bool new_state(PyObject* o, int32_t** p) const {
     *p = state;
@@ -620,7 +628,7 @@ struct Append {
           !vec(a[4], cache.c.batch + 1, at::kInt, false, &starts))
         return false;
     }
-    return (rest[0] == Py_None || rotary_of(rest[0])) && cache.new_state(rest[1], &new_state) && current_stream(&s);
+    return (rest[0] == Py_None || rotary_of(rest[0])) && cache.new_state(rest[1], &new_state) && cache.stream(&s);
   }
   bool rotary_of(PyObject* o) {
     bool none = false;
@@ -718,7 +726,7 @@ FUNCTION(cache_read, 5) {
       const at::Tensor* t = plain(l.o);
       NEED(t != nullptr && t->dim() == 1 && t->size(0) == l.n && vec(l.o, l.n, at::kInt, false, l.m));
     }
-  NEED(current_stream(&s));
+  NEED(cache.stream(&s));
   return status([&] {
     return abi.cache_read(&cache.c, cache.state, rows, (const int32_t*)starts.p, (const int32_t*)first.p, kt, k.p, k.ld,
                           v.p, v.ld, s);
@@ -750,7 +758,7 @@ FUNCTION(cache_attend, 7) {
     NEED(PyFloat_CheckExact(a[5]));
     scale = PyFloat_AS_DOUBLE(a[5]);
   }
-  NEED(truth(a[6], &accumulate) && (accumulate == 0 || cache.c.weights != nullptr) && current_stream(&s));
+  NEED(truth(a[6], &accumulate) && (accumulate == 0 || cache.c.weights != nullptr) && cache.stream(&s));
   // a call that is refused here is refused, with its message, by the Python code
   NEED(abi.cache_attend_workspace(&cache.c, (int32_t)heads, max_len, accumulate, &bytes) == MOSAIC_OK);
   return with_workspace(cache.device, bytes, [&](void* work) {
@@ -787,7 +795,7 @@ FUNCTION(cache_evict, 8) {
          t->size(1) == cache.c.kv_heads && t->size(2) == budget && t->is_contiguous() && t->data_ptr() != nullptr);
     kept = (int32_t*)t->data_ptr();
   }
-  NEED(current_stream(&s) && abi.cache_evict_workspace(&cache.c, max_len, budget, &bytes) == MOSAIC_OK);
+  NEED(cache.stream(&s) && abi.cache_evict_workspace(&cache.c, max_len, budget, &bytes) == MOSAIC_OK);
   return with_workspace(cache.device, bytes, [&](void* work) {
     return abi.cache_evict(&cache.c, cache.state, new_state, max_len, budget, recent, weights, order, kept, work, bytes, s);
   });

@@ -630,6 +630,11 @@ def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
             _device_tensor(t, f"cache.{name}", (dt,), 3)
             if t.shape != k.shape[:3] or not t.is_contiguous():
                 raise ValueError(f"cache.{name} must be a contiguous (pages, kv_heads, page_size) tensor")
+    if k.is_cuda and k.device.index != torch.cuda.current_device():
+        raise ValueError("the cache is on another device than the current one")
+    for name, t in (("v", v), ("block_table", table), ("state", cache.state), ("weights", cache.weights), ("order", cache.order)):
+        if t is not None and t.device != k.device:
+            raise ValueError(f"cache.{name} is on another device than cache.k")
     pages, heads, page, dim = k.shape
     if k.dtype == torch.uint8:
         if cache.head_dim is None or dim < KVCache.row_bytes(cache.head_dim):
@@ -645,6 +650,8 @@ def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
 
 def _cache_rows(t: torch.Tensor, rows: int, cols: int, name: str, cache: KVCache) -> None:
     _device_tensor(t, name, _FTYPE if cache.k.dtype == torch.uint8 else (torch.float32, cache.k.dtype), 2)
+    if t.device != cache.k.device:
+        raise ValueError(f"{name} is on another device than the cache")
     if t.shape[0] < rows or t.shape[1] < cols:
         raise ValueError(f"{name} is {tuple(t.shape)}, needs at least ({rows}, {cols})")
     if t.stride(1) != 1:
