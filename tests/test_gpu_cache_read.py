@@ -95,6 +95,15 @@ def test_a_prompt_and_many_sequences():
     check(c, eu, (3000,), "bf16")
 
 
+@pytest.mark.parametrize("dim,out", ((8, "f16"), (8, "f32"), (16, "f32"), (24, "bf16")))
+def test_short_rows(dim, out):
+    """Rows of a few 16-byte pieces, many of which a workgroup takes."""
+    lengths = (2500, 0, 1, 300)
+    c = eu.make_cache(lengths, 1, dim, 64, 15)
+    check(c, eu, lengths, out)
+    check(c, eu, (7, 0, 3, 290), out, firsts=(2490, 3, 0, 9))
+
+
 def test_shared_table_stream_and_graph():
     """A table row that all sequences share, on a side stream, captured and replayed."""
     c = eu.make_cache((50,), 2, 64, 16, 11)
