@@ -41,7 +41,7 @@
  * tokens are not read, not written and not evicted to. Sequences share no
  * page that a call writes to (through append, accumulated weights or
  * eviction). ``ldt`` 0 is one row of the table that all sequences share; only
- * attention without accumulated weights takes it.
+ * attention without accumulated weights, and reading, take it.
  *
  * ``state`` is an int32 array [2][batch]: the number of tokens that sequence
  * b holds (a negative one counts as 0, and one beyond the block table's
