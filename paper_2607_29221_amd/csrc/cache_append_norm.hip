@@ -12,7 +12,12 @@
 // fused: a key near the border of two codes then takes the one that the
 // formulas give, however they are computed.
 //
-// Bound by the traffic of the q|k|v rows.
+// Bound by the traffic of the q|k|v rows: 4096 tokens of 64 + 2 * 8 heads of 128 in
+// 35 to 38 us as bf16 (168 MB, 4.5 to 4.8 TB/s), in 63 to 70 us from float32 to 4
+// bits (309 MB, 4.4 to 4.9 TB/s). A single token takes 4.1 us, the latency of state,
+// page and table, one after the other, and of the root. Cosines, sines and weights
+// are read from LDS for every head: held in registers instead, their way there cost
+// more than a token's five rounds of heads got back (norms in bf16 55 us).
 #include "cache_append.h"
 #include "e2m1.h"
 
@@ -260,10 +265,11 @@ void launch_pairs(const AppendLaunch& a, int log2_lanes, hipStream_t s) {
   // Several tokens where a row is not long enough to cover the latency of finding
   // its token's place (4096 tokens of 80 heads of 128: bf16, 20 KiB each, 40.4 us
   // with one, 40.5 with two or three, 37.8 with four, 45 with eight; float32 into 4
-  // bits, 40 KiB each, 70 us with one, 72 with two, 73 with four), but two
-  // workgroups per compute unit at least.
+  // bits, 40 KiB each, 70 us with one, 72 with two, 73 with four), but four
+  // workgroups per compute unit at least (2048 tokens of 48 heads of 128: 14.2 us so,
+  // 17.4 with two, 15.8 with eight; 2224 of 10 heads of 256: 12.2, 15.1 and 12.9).
   const int64_t row = (a.heads + 2 * (int64_t)a.c.kv_heads) * a.c.head_dim * (XT == MOSAIC_F32 ? 4 : 2);
-  const int64_t share = THREADS == 1024 || row > 32768 ? 1 : a.rows / 512;
+  const int64_t share = THREADS == 1024 || row > 32768 ? 1 : a.rows / 1024;
   const int rows_of = share < 1 ? 1 : share > kMostRows ? kMostRows : (int)share;
   const dim3 grid((unsigned)((a.rows + rows_of - 1) / rows_of));
   if (a.rot.pairs == 0 || a.rot.interleaved)

@@ -311,6 +311,44 @@ def test_strided_rows():
     assert torch.equal(c.k, want.k) and torch.equal(c.v, want.v) and torch.equal(c.state, want.state)
 
 
+def test_nothing_new():
+    """No rows at all: only the state is handed on; no sequence: nothing is."""
+    c = eu.make_cache((3, 4), 2, 64, 16, 69)
+    old, state = eu.clone(c), torch.full_like(c.state, -1)
+    w = torch.ones(64, device="cuda")
+    x, q = torch.empty((0, 8 * 64), device="cuda"), torch.empty((0, 256), device="cuda")
+    m.mosaic_cache_append_norm(c, x, 4, q, m.QKNorm(w, w), starts=torch.zeros(3, dtype=torch.int32, device="cuda"),
+                               new_state=state)
+    assert torch.equal(state, old.state) and torch.equal(c.k, old.k) and torch.equal(c.v, old.v)
+    none = eu.make_cache((), 2, 64, 16, 70)
+    m.mosaic_cache_append_norm(none, x, 4, q, m.QKNorm(w, w))
+    m.mosaic_cache_attend(none, q, 4, torch.empty_like(q))
+    m.mosaic_cache_read(none, torch.empty((0, 128), device="cuda"), torch.empty((0, 128), device="cuda"))
+
+
+def test_state_elsewhere_with_starts():
+    """Ragged tokens with the new state in another tensor, several tokens to a workgroup."""
+    fresh = (700, 0, 900, 3)
+    c = eu.make_cache((5, 9, 0, 30), 2, 64, 64, 71, room=900)
+    old, state = eu.clone(c), torch.full_like(c.state, -1)
+    args = inputs(c, 64, 4, "bf16", fresh, ((32,), False), 72, text=True, table_rows=1000)
+    call(c, 4, *args, new_state=state)
+    x, q, n, _, rotary = args
+    assert torch.equal(state, check(c, old, 4, 64, "bf16", fresh, x, q, n, rotary, eu)) and torch.equal(c.state, old.state)
+
+
+def test_many_sequences_of_one_token():
+    """More sequences than a workgroup per compute unit, no starts, state in place."""
+    batch = 1300
+    lengths = [int(i) for i in np.random.default_rng(5).integers(0, 40, batch)]
+    c = eu.make_cache(lengths, 1, 16, 16, 73, room=1)
+    old = eu.clone(c)
+    args = inputs(c, 16, 2, "f16", (1,) * batch, ((8,), False), 74, starts=False, text=True)
+    call(c, 2, *args)
+    x, q, n, _, rotary = args
+    assert torch.equal(c.state, check(c, old, 2, 16, "f16", (1,) * batch, x, q, n, rotary, eu))
+
+
 @pytest.mark.parametrize("four", (False, True))
 def test_graph_of_a_step(four):
     """Captured with the state in place, on a stream of its own: every replay is
