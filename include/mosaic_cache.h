@@ -17,6 +17,8 @@
  * Conventions are those of mosaic.h (device pointers owned by the caller,
  * asynchronous on ``stream``, arguments validated before anything is
  * launched, nothing allocated or kept between calls, empty calls do nothing).
+ * All memory of a call lies on one device, which is the stream's and the
+ * current one (the Python functions check that).
  * Workspaces are the caller's too: their sizes come from the *_workspace
  * functions, their contents have no meaning between calls, and two calls that
  * may run at the same time need one each. 16-byte alignment is required

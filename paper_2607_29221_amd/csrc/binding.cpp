@@ -580,8 +580,15 @@ struct Cache {
     const at::Tensor* t = plain(o);
     if (t == nullptr || (t->scalar_type() != at::kFloat && t->scalar_type() != dtype && !four)) return false;
     *type = ftype(t->scalar_type());
-    if (*type < 0 || t->device() != device) return false;
+    if (*type < 0 || !here(t)) return false;
     return matrix(o, n, cols, t->scalar_type(), false, m);
+  }
+  bool here(const at::Tensor* t) const { return t->device() == device; }
+  // int32 entries, as many as they should be, or None
+  bool list(PyObject* o, int64_t n, Mat* m) const {
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o);
+    return t != nullptr && here(t) && t->dim() == 1 && t->size(0) == n && vec(o, n, at::kInt, false, m);
   }
   // the current stream, of the device that the cache is on
   bool stream(void** s) const {
@@ -592,7 +599,7 @@ struct Cache {
     *p = state;
     if (o == Py_None) return true;
     const at::Tensor* t = plain(o);
-    if (t == nullptr || !state_like(t)) return false;
+    if (t == nullptr || !here(t) || !state_like(t)) return false;
     *p = (int32_t*)t->data_ptr();
     return *p != nullptr;
   }
@@ -622,19 +629,14 @@ struct Append {
     if (!cache.rows(a[1], rows, (heads + 2 * (int64_t)cache.c.kv_heads) * D, &xt, &x) ||
         !cache.rows(a[3], rows, heads * D, &qt, &q) || xt != qt)
       return false;
-    if (a[4] != Py_None) {
-      const at::Tensor* t = plain(a[4]);
-      if (t == nullptr || t->dim() != 1 || t->size(0) != cache.c.batch + 1 ||
-          !vec(a[4], cache.c.batch + 1, at::kInt, false, &starts))
-        return false;
-    }
-    return (rest[0] == Py_None || rotary_of(rest[0])) && cache.new_state(rest[1], &new_state) && cache.stream(&s);
+    return cache.list(a[4], (int64_t)cache.c.batch + 1, &starts) && (rest[0] == Py_None || rotary_of(rest[0])) &&
+           cache.new_state(rest[1], &new_state) && cache.stream(&s);
   }
   bool rotary_of(PyObject* o) {
     bool none = false;
     const at::Tensor *table = attr(o, s_table, 2, &held[0]), *positions = attr(o, s_positions, 2, &held[1], &none);
     if (table == nullptr || table->scalar_type() != at::kFloat || !table->is_contiguous() || table->size(0) == 0) return false;
-    if (positions == nullptr && !none) return false;
+    if ((positions == nullptr && !none) || !cache.here(table) || (positions != nullptr && !cache.here(positions))) return false;
     PyObject* sections = PyObject_GetAttr(o, s_sections);
     int64_t pairs = 0;
     bool ok = sections != nullptr && (PyList_CheckExact(sections) || PyTuple_CheckExact(sections));
@@ -688,7 +690,7 @@ FUNCTION(cache_append_norm, 8) {
   mosaic_qk_norm norm{};
   const at::Tensor *qw = attr(a[4], s_q_weight, 1, &held[0]), *kw = attr(a[4], s_k_weight, 1, &held[1]);
   for (const at::Tensor* w : {qw, kw})
-    NEED(w != nullptr && w->scalar_type() == at::kFloat && w->size(0) == p.cache.c.head_dim && w->stride(0) == 1);
+    NEED(w != nullptr && p.cache.here(w) && w->scalar_type() == at::kFloat && w->size(0) == p.cache.c.head_dim && w->stride(0) == 1);
   PyObject* const eps = PyObject_GetAttr(a[4], s_eps);
   const bool ok = eps != nullptr && PyFloat_CheckExact(eps);
   if (ok) norm.eps = (float)PyFloat_AS_DOUBLE(eps);
@@ -716,17 +718,7 @@ FUNCTION(cache_read, 5) {
        vten->size(0) == kten->size(0));
   const int64_t rows = kten->size(0), width = (int64_t)cache.c.kv_heads * cache.c.head_dim;
   NEED(cache.rows(a[1], rows, width, &kt, &k) && cache.rows(a[2], rows, width, &vt, &v) && kt == vt);
-  const struct {
-    PyObject* o;
-    int64_t n;
-    Mat* m;
-  } lists[] = {{a[3], (int64_t)cache.c.batch + 1, &starts}, {a[4], cache.c.batch, &first}};
-  for (const auto& l : lists)
-    if (l.o != Py_None) {
-      const at::Tensor* t = plain(l.o);
-      NEED(t != nullptr && t->dim() == 1 && t->size(0) == l.n && vec(l.o, l.n, at::kInt, false, l.m));
-    }
-  NEED(cache.stream(&s));
+  NEED(cache.list(a[3], (int64_t)cache.c.batch + 1, &starts) && cache.list(a[4], cache.c.batch, &first) && cache.stream(&s));
   return status([&] {
     return abi.cache_read(&cache.c, cache.state, rows, (const int32_t*)starts.p, (const int32_t*)first.p, kt, k.p, k.ld,
                           v.p, v.ld, s);
@@ -781,17 +773,17 @@ FUNCTION(cache_evict, 8) {
   int32_t *order = cache.c.order, *kept = nullptr;
   if (a[5] != Py_None) {
     const at::Tensor* t = plain(a[5]);
-    NEED(t != nullptr && cache.numbers(t, at::kFloat));
+    NEED(t != nullptr && cache.here(t) && cache.numbers(t, at::kFloat));
     weights = (float*)t->data_ptr();
   }
   if (a[6] != Py_None) {
     const at::Tensor* t = plain(a[6]);
-    NEED(t != nullptr && cache.numbers(t, at::kInt));
+    NEED(t != nullptr && cache.here(t) && cache.numbers(t, at::kInt));
     order = (int32_t*)t->data_ptr();
   }
   if (a[7] != Py_None) {
     const at::Tensor* t = plain(a[7]);
-    NEED(t != nullptr && t->scalar_type() == at::kInt && t->dim() == 3 && t->size(0) == cache.c.batch &&
+    NEED(t != nullptr && cache.here(t) && t->scalar_type() == at::kInt && t->dim() == 3 && t->size(0) == cache.c.batch &&
          t->size(1) == cache.c.kv_heads && t->size(2) == budget && t->is_contiguous() && t->data_ptr() != nullptr);
     kept = (int32_t*)t->data_ptr();
   }

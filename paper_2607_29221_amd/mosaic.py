@@ -528,7 +528,11 @@ class KVCache:
     how many tokens it holds and how many it has seen. ``weights`` (float32)
     and ``order`` (int32), contiguous (pages, kv_heads, page_size), are needed
     for eviction only. In 4 bits (uint8 tensors) the last dimension is a row's
-    bytes, row_bytes(head_dim) or more, and ``head_dim`` must be given."""
+    bytes, row_bytes(head_dim) or more, and ``head_dim`` must be given.
+
+    The functions over a cache run on the current stream. All tensors of a call
+    lie on its device, the current one; a call with one elsewhere raises
+    ValueError."""
     k: torch.Tensor
     v: torch.Tensor
     block_table: torch.Tensor
@@ -609,6 +613,11 @@ def _device_tensor(t, name: str, dtypes, dim: int) -> None:
         raise ValueError(f"{name} must have {dim} dimensions")
 
 
+def _here(t: torch.Tensor, name: str, cache: KVCache) -> None:
+    if t.device != cache.k.device:
+        raise ValueError(f"{name} is on another device than the cache")
+
+
 def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
     """The C struct of a cache whose tensors fit together."""
     k, v, table = cache.k, cache.v, cache.block_table
@@ -650,20 +659,20 @@ def _cache_arg(cache: KVCache) -> _lib.MosaicKvCache:
 
 def _cache_rows(t: torch.Tensor, rows: int, cols: int, name: str, cache: KVCache) -> None:
     _device_tensor(t, name, _FTYPE if cache.k.dtype == torch.uint8 else (torch.float32, cache.k.dtype), 2)
-    if t.device != cache.k.device:
-        raise ValueError(f"{name} is on another device than the cache")
+    _here(t, name, cache)
     if t.shape[0] < rows or t.shape[1] < cols:
         raise ValueError(f"{name} is {tuple(t.shape)}, needs at least ({rows}, {cols})")
     if t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
 
 
-def _same_shape(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: str) -> Optional[torch.Tensor]:
+def _same_shape(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: str, cache: KVCache) -> Optional[torch.Tensor]:
     if t is None:
         return like
     if like is None:
         raise ValueError(f"{name} has no counterpart in the cache")
     _device_tensor(t, name, (like.dtype,), like.dim())
+    _here(t, name, cache)
     if t.shape != like.shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {tuple(like.shape)} tensor")
     return t
@@ -681,19 +690,22 @@ def _append_args(cache: KVCache, qkv: torch.Tensor, heads: int, q_out: torch.Ten
         raise ValueError("q_out must have the type of qkv")
     if starts is not None:
         _device_tensor(starts, "starts", _INT, 1)
+        _here(starts, "starts", cache)
         if starts.shape[0] != c.batch + 1 or starts.stride(0) != 1:
             raise ValueError("starts must be a contiguous vector of batch + 1 entries")
-    state = _same_shape(new_state, cache.state, "new_state")
+    state = _same_shape(new_state, cache.state, "new_state", cache)
     r = None
     if rotary is not None:
         sections = [int(n) for n in rotary.sections]
         if not 1 <= len(sections) <= 4:
             raise ValueError("rotary positions have one to four axes")
         _device_tensor(rotary.table, "rotary.table", (torch.float32,), 2)
+        _here(rotary.table, "rotary.table", cache)
         if rotary.table.shape[1] != 2 * sum(sections) or not rotary.table.is_contiguous():
             raise ValueError("rotary.table must be contiguous, with a cosine and a sine for every pair")
         if rotary.positions is not None:
             _device_tensor(rotary.positions, "rotary.positions", _INT, 2)
+            _here(rotary.positions, "rotary.positions", cache)
             if rotary.positions.shape[0] < len(sections) or rotary.positions.shape[1] < rows or \
                     (rows > 1 and rotary.positions.stride(1) != 1):
                 raise ValueError("rotary.positions must hold a row of places for every axis")
@@ -733,6 +745,7 @@ def mosaic_cache_append_norm(cache: KVCache, qkv: torch.Tensor, heads: int, q_ou
     dim = cache.head_dim if cache.k.dtype == torch.uint8 else cache.k.shape[3]
     for name, w in (("q_weight", norm.q_weight), ("k_weight", norm.k_weight)):
         _device_tensor(w, f"norm.{name}", (torch.float32,), 1)
+        _here(w, f"norm.{name}", cache)
         if w.shape[0] != dim or not w.is_contiguous():
             raise ValueError(f"norm.{name} must be a contiguous vector of head_dim entries")
     w = _lib.MosaicQkNorm(q_weight=_ptr(norm.q_weight), k_weight=_ptr(norm.k_weight), eps=norm.eps)
@@ -757,6 +770,7 @@ def mosaic_cache_read(cache: KVCache, k_out: torch.Tensor, v_out: torch.Tensor, 
     for name, t, n in (("starts", starts, c.batch + 1), ("first", first, c.batch)):
         if t is not None:
             _device_tensor(t, name, _INT, 1)
+            _here(t, name, cache)
             if t.shape[0] != n or (n > 1 and t.stride(0) != 1):
                 raise ValueError(f"{name} must be a contiguous vector of {n} entries")
     _check(_lib.load().mosaic_cache_read(ctypes.byref(c), _ptr(cache.state), rows, _ptr(starts), _ptr(first),
@@ -807,11 +821,12 @@ def mosaic_cache_evict(cache: KVCache, budget: int, recent: int, max_len: Option
     c = _cache_arg(cache)
     if cache.weights is None or cache.order is None:
         raise ValueError("eviction needs a cache with weights and order")
-    state = _same_shape(new_state, cache.state, "new_state")
-    weights = _same_shape(new_weights, cache.weights, "new_weights")
-    order = _same_shape(new_order, cache.order, "new_order")
+    state = _same_shape(new_state, cache.state, "new_state", cache)
+    weights = _same_shape(new_weights, cache.weights, "new_weights", cache)
+    order = _same_shape(new_order, cache.order, "new_order", cache)
     if kept is not None:
         _device_tensor(kept, "kept", _INT, 3)
+        _here(kept, "kept", cache)
         if tuple(kept.shape) != (c.batch, c.kv_heads, budget) or not kept.is_contiguous():
             raise ValueError("kept must be a contiguous (batch, kv_heads, budget) tensor")
     n = cache.slots if max_len is None else max_len
