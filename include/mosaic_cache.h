@@ -180,9 +180,10 @@ mosaic_status mosaic_cache_read(const mosaic_kv_cache* cache, const int32_t* len
  *     out_g = sum_i p_i v_i,
  * zeros for a sequence without tokens. Infinities and NaN among the tokens act
  * as in these formulas (a score of -inf is no weight; zeros if there is no
- * other). Scores, softmax sums and outputs are accumulated in float32, outputs
- * before the division and with weights of up to 2^8: a value above 2^119 over
- * the number of tokens may overflow there. ``accumulate`` nonzero adds p_i of
+ * other; q_g . k_i beyond the range of float32 is infinite). Scores, softmax
+ * sums and outputs are accumulated in float32, outputs before the division and
+ * with weights of up to 2^8: a value above 2^119 over the number of tokens may
+ * overflow there. ``accumulate`` nonzero adds p_i of
  * every head of the group to ``weights`` of slot i and head h (without atomics:
  * two runs give the same bits). q and out are batch x heads * head_dim of
  * x_dtype (MOSAIC_F32 or the cache's type, any of the three over 4 bits), 16-byte aligned, ldq and ldo

@@ -402,6 +402,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
         }
 
       float dot[NT][F::kRows], tile_top[NT];
+      // the largest score of a lane, NaN if one is NaN
+      auto tops = [&](int nt) {
+        tile_top[nt] = dot[nt][0];
+#pragma unroll
+        for (int i = 1; i < F::kRows; ++i) tile_top[nt] = __builtin_elementwise_maximum(tile_top[nt], dot[nt][i]);
+        tile_top[nt] *= scale;
+      };
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         f32x4 d[F::kSub];
@@ -431,10 +438,25 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        tile_top[nt] = dot[nt][0];
+        tops(nt);
+        // The products of two parts of a query may overflow to infinities of both
+        // signs and add up to NaN although the sum is infinite: such a score is taken
+        // from the first parts alone, which have the sign of the whole.
+        if (PARTS > 1 && __any(tile_top[nt] != tile_top[nt])) {
+          f32x4 d[F::kSub];
 #pragma unroll
-        for (int i = 1; i < F::kRows; ++i) tile_top[nt] = fmaxf(tile_top[nt], dot[nt][i]);
-        tile_top[nt] *= scale;
+          for (int s = 0; s < F::kSub; ++s) d[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < KL; ++c)
+#pragma unroll
+            for (int s = 0; s < F::kSub; ++s) d[s] = mul(kf[s][c], query[nt][0][c][lane], d[s]);
+#pragma unroll
+          for (int i = 0; i < F::kRows; ++i) {
+            const float x = R > 1 ? __shfl(d[i / 4][i % 4], 16 * quad + col % W) : d[i / 4][i % 4];
+            dot[nt][i] = dot[nt][i] == dot[nt][i] ? dot[nt][i] : x;
+          }
+          tops(nt);
+        }
       }
       if (a.accumulate) {
         if (4 * held_heads * (holding + F::kSub) > kHold) release();
