@@ -85,7 +85,9 @@ struct Plan {
   int32_t wave_tiles, tile_groups;        // blocks of 16 query heads of a group: per wave, and so many times
 };
 
-Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
+// two_fit: whether a unit's LDS holds two workgroups; there are never more of them
+// without than with it (which the workspace is sized for).
+Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len, bool two_fit = true) {
   Plan p;
   const int32_t tiles = (heads / c.kv_heads + kHeadTile - 1) / kHeadTile;
   // two blocks share a wave's keys and values where the registers hold both outputs
@@ -104,8 +106,10 @@ Plan plan_of(const CacheView& c, int32_t heads, int64_t max_len) {
   // with 264, 173 us with 252), but more per unit where more than one unit in 16
   // would idle (71 heads: 217 us with 213, 186 us with 497). Over 4 bits, where the
   // arithmetic takes as long as the rows, two per unit as long as its LDS holds them
-  // (131072 tokens of 32 and 8 heads: 39 us with 256 in all, 35 with 512, 37.5 with 768).
-  const bool two = c.head_dim <= 128 && (p.tile_groups > 1 || c.dtype == MOSAIC_E2M1);
+  // (131072 tokens of 32 and 8 heads: 39 us with 256 in all, 35 with 512, 37.5 with 768),
+  // which with float32 activations, weights and blocks of 32 heads it does not (32 heads
+  // on one: one sequence of 131072 66 us with 512, 47 with 256, 32 of up to 7168 59 and 51).
+  const bool two = two_fit && c.head_dim <= 128 && (p.tile_groups > 1 || c.dtype == MOSAIC_E2M1);
   int32_t slots = two ? 512 : 256;
   int64_t wanted;
   while (true) {

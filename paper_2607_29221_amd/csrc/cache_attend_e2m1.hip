@@ -126,7 +126,14 @@ template <int XT, int DP, int NT, int W> struct Lds {
     const int in = kQuery + kRows + kPast + (accumulate ? kWaves * kHold * 16 : 0);
     return in > kSlab ? in : kSlab;
   }
+  static constexpr int kStat = NT * kWaves * kHeadTile * 8;
+  static constexpr bool two_fit(bool accumulate) { return 2 * (bytes(accumulate) + kStat) <= 160 * 1024; }
 };
+
+// Whether a unit holds two workgroups of a call (parts side by side take less LDS).
+template <int XT, int DP> bool two_fit(const AttendLaunch& a) {
+  return a.heads / a.c.kv_heads > kHeadTile ? Lds<XT, DP, 2, 16>::two_fit(a.accumulate) : Lds<XT, DP, 1, 16>::two_fit(a.accumulate);
+}
 
 // NT: blocks of 16 query heads per wave. W: where a group has at most 8 or 4
 // heads, columns W, 2W, ... of a block hold further parts of the heads in the first
@@ -651,8 +658,13 @@ void launch_dim(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t
 }
 
 template <int XT>
+Plan plan_for(const AttendLaunch& a) {
+  return plan_of(a.c, a.heads, a.max_len, a.c.head_dim <= 64 ? two_fit<XT, 64>(a) : a.c.head_dim <= 128 && two_fit<XT, 128>(a));
+}
+
+template <int XT>
 hipError_t launch_types(const AttendLaunch& a, hipStream_t s) {
-  const Plan p = plan_of(a.c, a.heads, a.max_len);
+  const Plan p = plan_for<XT>(a);
   const Work w = work_of(a, p);
   if (a.c.head_dim <= 64) launch_dim<XT, 64>(a, w, p, s);
   else if (a.c.head_dim <= 128) launch_dim<XT, 128>(a, w, p, s);
