@@ -76,7 +76,8 @@ def row_bytes(dim):
 def to_e2m1(x):
     """Codes (... x dim) and scales (... x dim / 8) of x: the least power of two
     from 2^-126 to 2^125 under which no magnitude of 8 is over 7, the nearest
-    codes, an even one between two; scale 255 where one is not finite."""
+    codes with the sign of x (of a zero too), an even one between two; scale 255
+    where one is not finite."""
     x = np.asarray(x, dtype=np.float64)
     g = x.reshape(*x.shape[:-1], x.shape[-1] // 8, 8)
     top = np.abs(g).max(axis=-1)
@@ -90,7 +91,7 @@ def to_e2m1(x):
     far = np.abs(a[..., None] - E2M1)
     best = far.min(axis=-1, keepdims=True)
     order = np.array([0, 2, 4, 6, 1, 3, 5, 7])          # even codes first
-    code = order[np.argmax(far[..., order] == best, axis=-1)] + 8 * (g < 0)
+    code = order[np.argmax(far[..., order] == best, axis=-1)] + 8 * np.signbit(g)
     return np.where(fine[..., None], code, 0).reshape(x.shape), scale
 
 

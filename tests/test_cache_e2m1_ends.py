@@ -1,0 +1,57 @@
+"""The ends of a cache in 4 bits: where a scale can get no smaller (2^-126) and no
+larger (2^125): bytes as the oracle has them, the sign of a zero too."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as oc
+from paper_2607_29221_amd import mosaic as m
+from tests import e2m1_util as eu
+from tests.cache_util import DT, f64, same_bits
+
+LOW, HIGH = 2.0 ** -126, 2.0 ** 125
+# largest of the 8, in units of the smallest and of the largest scale
+LOW_TOPS = (2.0 ** -23, 0.1, 0.2499, 0.25, 0.2501, 0.5, 0.75, 1.0, 1.25, 3.0, 5.0, 6.99, 7.0, 7.01, 13.9, 14.0, 14.1, 28.0)
+HIGH_TOPS = (0.87, 1.74, 1.75, 1.76, 3.5, 3.51, 5.0, 6.0, 6.9, 7.0, 7.01, 7.5, 7.99)
+
+
+def rows(dtype=torch.float32):
+    """Groups of 8 whose largest are the ones above, the others spread below, as
+    far down as 1/64 of it and 0; of either sign."""
+    parts = np.array([1.0, -0.9, 0.71, -0.5, 0.36, -0.2, 0.0157, 0.0])
+    x = np.concatenate([np.outer(LOW_TOPS, parts) * LOW, np.outer(HIGH_TOPS, parts) * HIGH])
+    x = torch.from_numpy(np.concatenate([x, -x])).to(dtype)
+    top = torch.finfo(dtype).max
+    return torch.cat([x, torch.full((1, 8), top, dtype=dtype), torch.full((1, 8), torch.finfo(dtype).smallest_normal, dtype=dtype)])
+
+
+def test_signs_of_zeros():
+    x = np.array([[0.0, -0.0, 1.0, -1.0, 0.01, -0.01, -0.0, 0.0], [-0.0] * 8])
+    codes, scales = oc.to_e2m1(x)
+    assert scales[:, 0].tolist() == [125, 1] and (codes >= 8).tolist() == np.signbit(x).tolist()
+    y = oc.unpack_e2m1(oc.pack_e2m1(codes, scales), 8)
+    assert np.array_equal(np.signbit(y), np.signbit(x))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", eu.ACTS)
+def test_bytes_at_the_ends(act):
+    """Appended as values, without norm or rotation: the oracle's bytes. f16 has
+    only the middle of the range, and its own ends."""
+    x = rows(DT[act]) if act != "f16" else torch.cat([rows(DT[act])[-2:], torch.tensor([[2.0 ** -24, -2.0 ** -24, 3 * 2.0 ** -24, 0.0, 65504.0, 1.0, -60000.0, 5e-5],
+                                                                                        [2.0 ** -24, -2.0 ** -23, 3 * 2.0 ** -24, 0, 0, 0, 0, 0]], dtype=DT[act])])
+    n = len(x)
+    c = eu.make_cache((0,), 1, 8, 64, 5, room=n)
+    qkv = torch.cat([torch.zeros((n, 8), dtype=DT[act]), x, x.flip(0)], dim=1).cuda()
+    q = torch.empty((n, 8), dtype=DT[act], device="cuda")
+    m.mosaic_cache_append(c, qkv, 1, q, starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    used = 8 // 2 + 1
+    for name, want in (("k", x), ("v", x.flip(0))):
+        held = oc.pack_e2m1(*oc.to_e2m1(f64(want)))
+        got = eu.rows_of(c, name, 0, 0, n)[0]
+        assert np.array_equal(got[:, :used], held[:, :used]), np.nonzero((got != held)[:, :used].any(axis=1))
+        for out in eu.ACTS:
+            k, v = (torch.empty((n, 8), dtype=DT[out], device="cuda") for _ in range(2))
+            m.mosaic_cache_read(c, k, v, starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+            exact = torch.from_numpy(oc.unpack_e2m1(held, 8))
+            assert same_bits((k if name == "k" else v).cpu(), exact.to(DT[out])), out
