@@ -76,11 +76,14 @@ typedef enum mosaic_ftype {
  * written nor read, except by eviction, which moves whole rows). A code is a
  * sign (8) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 to 7); a scale e
  * multiplies by 2^(e - 127), and 255 makes all 8 elements NaN. What is written:
- * e is the smallest from 1 on that leaves no magnitude over 7 (252 at most,
- * where magnitudes over 2^125 * 7 become 2^125 * 6), codes are the nearest, an
- * even one between two: an element is off by at most half the distance of the
- * codes around it (1 beyond 6), which is a fifth of the largest of its 8 or less.
- * 8 elements with an infinity or NaN among them become NaN.
+ * e is the smallest from 1 on that leaves no magnitude over 7 (252 at most),
+ * codes are the nearest, an even one between two, with the element's sign (a
+ * zero's too). An element is off by at most half the distance of the codes
+ * around it (1 beyond 6), which is a fifth of the largest of its 8, or 2^-128
+ * if that is more. Where e would have to be over 252, magnitudes over 2^125 * 7
+ * become 2^125 * 6: off by a quarter of themselves at most. 8 elements with an
+ * infinity or NaN among them become NaN. Scales of 0, 253 and 254 are never
+ * written; rows that a caller writes itself have none either.
  * The strides of such a cache are in bytes. */
 #define MOSAIC_E2M1_ROW_BYTES(head_dim) (((head_dim) / 2 + (head_dim) / 8 + 15) / 16 * 16)
 
@@ -148,8 +151,10 @@ mosaic_status mosaic_cache_append(const mosaic_kv_cache* cache, const void* qkv,
  * float64 and rounded to a float32 factor; from there on each product and sum
  * of the element and of its rotation is rounded to float32 by itself (nothing
  * is fused), here and wherever the cache is in 4 bits: a key between two codes
- * takes the same one in any computation of these formulas. eps >= 0, finite; the
- * weights lie in none of the outputs. */
+ * takes the same one in any computation of these formulas, but for about one
+ * head in 2^26, whose factor lies so near the border of two float32 numbers that
+ * the rounding of the float64 sum decides. eps >= 0, finite; the weights lie in
+ * none of the outputs. */
 typedef struct mosaic_qk_norm {
   const float* q_weight;      /* head_dim entries each, 4-byte aligned */
   const float* k_weight;

@@ -1,5 +1,7 @@
 """The ends of a cache in 4 bits: where a scale can get no smaller (2^-126) and no
-larger (2^125): bytes as the oracle has them, the sign of a zero too."""
+larger (2^125). Bytes as the oracle has them, and how far an element may be off:
+half the distance of the codes around it, a fifth of the largest of its 8 or 2^-128
+if that is more; above 2^125 * 7, where 2^125 * 6 is the last, a quarter."""
 import numpy as np
 import pytest
 import torch
@@ -23,6 +25,30 @@ def rows(dtype=torch.float32):
     x = torch.from_numpy(np.concatenate([x, -x])).to(dtype)
     top = torch.finfo(dtype).max
     return torch.cat([x, torch.full((1, 8), top, dtype=dtype), torch.full((1, 8), torch.finfo(dtype).smallest_normal, dtype=dtype)])
+
+
+def test_oracle_at_the_ends():
+    x = rows().double().numpy()
+    codes, scales = oc.to_e2m1(x)
+    y = oc.unpack_e2m1(oc.pack_e2m1(codes, scales), 8)
+    top = np.abs(x).max(axis=-1, keepdims=True)
+    off = np.abs(x - y)
+    below = (top <= 7.0 * HIGH)[:, 0]
+    assert (off[below] <= np.maximum(0.2 * top, 2.0 ** -128)[below]).all()
+    assert (off[~below] <= 0.25 * top[~below]).all() and (scales[~below] == 252).all()
+    a = np.abs(x) / 2.0 ** (scales - 127.0)
+    step = np.where(a <= 2.0, 0.25, np.where(a <= 4.0, 0.5, np.where(a <= 7.0, 1.0, 2.0)))
+    assert (off <= step * 2.0 ** (scales - 127.0)).all()
+    # the bounds are met: all of it is lost below a quarter of the smallest scale, a fourth at the top
+    assert (off[below] > 0.9 * top[below]).any() and (off[~below] > 0.245 * top[~below]).any()
+    assert scales.min() == 1 and scales.max() == 252
+
+
+def test_a_clamped_largest_by_hand():
+    x = np.array([[1.9 * 2.0 ** 127] + [2.0 ** -130] * 7, [2.0 ** -130] * 8, [2.0 ** -127] * 8, [2.0 ** -128] * 4 + [-1.5 * 2.0 ** -128] * 4])
+    codes, scales = oc.to_e2m1(x)
+    assert scales[:, 0].tolist() == [252, 1, 1, 1]
+    assert codes.tolist() == [[7] + [0] * 7, [0] * 8, [1] * 8, [0] * 4 + [9] * 4]
 
 
 def test_signs_of_zeros():
