@@ -173,7 +173,8 @@ mosaic_status mosaic_cache_append_norm(const mosaic_kv_cache* cache, const void*
  * out_dtype has fewer bits than they need. A slot that holds no token (below 0,
  * at or past lengths[b], or on a page that is not there) gives zeros. k_out and
  * v_out 16-byte aligned, ldk and ldv multiples of 16 bytes, overlapping neither
- * each other nor the cache. */
+ * each other (with one stride they may lie side by side, as columns of a matrix)
+ * nor the cache. */
 mosaic_status mosaic_cache_read(const mosaic_kv_cache* cache, const int32_t* lengths, int64_t rows,
                                 const int32_t* starts, const int32_t* first, int32_t out_dtype, void* k_out,
                                 int64_t ldk, void* v_out, int64_t ldv, void* stream);

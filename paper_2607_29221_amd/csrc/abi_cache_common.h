@@ -20,6 +20,16 @@ inline bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
 // Bytes from the first to the last element of rows x cols.
 inline int64_t extent(int64_t rows, int64_t ld, int64_t cols, int64_t size) { return ((rows - 1) * ld + cols) * size; }
 
+// Whether `rows` rows of an bytes and as many of bn bytes overlap; rows as far apart
+// in both may lie side by side.
+inline bool rows_overlap(const void* a, int64_t lda, int64_t an, const void* b, int64_t ldb, int64_t bn, int64_t rows) {
+  if (!overlap(a, (rows - 1) * lda + an, b, (rows - 1) * ldb + bn)) return false;
+  if (lda != ldb) return true;
+  const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  const int64_t at = (apart % lda + lda) % lda;      // where the one's rows begin, from the other's
+  return at < an || at + bn > lda;
+}
+
 inline mosaic_status view_of(const mosaic_kv_cache* c, CacheView* v) {
   if (c == nullptr) return fail(MOSAIC_ERR_INVALID_ARG, "cache is NULL");
   if ((c->dtype < MOSAIC_F32 || c->dtype > MOSAIC_F16) && c->dtype != MOSAIC_E2M1)

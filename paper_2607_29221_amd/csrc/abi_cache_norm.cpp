@@ -34,7 +34,8 @@ mosaic_status mosaic_cache_read(const mosaic_kv_cache* cache, const int32_t* len
   if ((st = check_rows(k_out, rows, ldk, width, size, "k_out")) != MOSAIC_OK) return st;
   if ((st = check_rows(v_out, rows, ldv, width, size, "v_out")) != MOSAIC_OK) return st;
   const int64_t kn = extent(rows, ldk, width, size), vn = extent(rows, ldv, width, size);
-  if (overlap(k_out, kn, v_out, vn)) return fail(MOSAIC_ERR_INVALID_ARG, "k_out overlaps v_out");
+  if (rows_overlap(k_out, ldk * size, width * size, v_out, ldv * size, width * size, rows))
+    return fail(MOSAIC_ERR_INVALID_ARG, "k_out overlaps v_out");
   if (a.c.pages > 0) {
     const int64_t row = a.c.dtype == MOSAIC_E2M1 ? MOSAIC_E2M1_ROW_BYTES(a.c.head_dim) : a.c.head_dim * size_of(a.c.dtype);
     const int64_t held = (a.c.pages - 1) * a.c.page_stride + (a.c.kv_heads - 1) * a.c.head_stride +
