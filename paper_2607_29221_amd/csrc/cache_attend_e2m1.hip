@@ -325,8 +325,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
       for (int i = 0; i < NT * PASSES * KL; ++i) kept[i] = (&query[0][0][0][0])[64 * i + lane];
     }
     f32x4 acc[NT][NV][EV];
-    float top[NT], base[NT];
-    f32x4 sum[NT];                              // of the weights: their products with ones
+    float top[NT], base[NT], sum[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -334,8 +333,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
 #pragma unroll
         for (int j = 0; j < EV; ++j) acc[nt][v][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       top[nt] = -INFINITY;
-      base[nt] = 0.0f;
-      sum[nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      base[nt] = sum[nt] = 0.0f;
     }
 
     // Scores go to memory through LDS, many steps at a time.
@@ -497,6 +495,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
 #pragma unroll
         for (int i = 0; i < F::kRows; i += 2) {
           const float w0 = exp2_fast(fmaf(dot[nt][i], scale, -base[nt])), w1 = exp2_fast(fmaf(dot[nt][i + 1], scale, -base[nt]));
+          sum[nt] += w0 + w1;                     // all of them, whatever their parts leave out
           uint32_t part[WPARTS];
           split_pair<WPARTS>(w0, w1, part);
 #pragma unroll
@@ -509,12 +508,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
         }
       }
 
-      const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-#pragma unroll
-      for (int part = WPASSES - 1; part >= 0; --part)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          sum[nt] = mul(__builtin_bit_cast(Frag, ones), __builtin_bit_cast(Frag, pf[nt][part]), sum[nt]);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         uint32_t x[F::kRows][EV / 2];               // pairs of a token's columns
@@ -563,9 +556,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2
     const int own_col = own_lane & 15, own_quad = own_lane >> 4;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float all = sum[nt][0];                     // of this column's parts: the same in all rows
-      if (R > 1) all += other_column<8>(all);
-      if (R > 2) all += other_column<4>(all);
+      const float all = head_sum(sum[nt]);        // the same in all columns of a head
       if (own_quad == 0) {
         stat[nt][wave][own_col][0] = top[nt] == -INFINITY ? -INFINITY : base[nt];
         stat[nt][wave][own_col][1] = all;
