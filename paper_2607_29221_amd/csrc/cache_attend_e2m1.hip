@@ -137,8 +137,7 @@ template <int XT, int DP> bool two_fit(const AttendLaunch& a) {
 
 // NT: blocks of 16 query heads per wave. W: where a group has at most 8 or 4
 // heads, columns W, 2W, ... of a block hold further parts of the heads in the first
-// W, so that a product takes several parts at a time (64 sequences, 64 query and 8
-// key/value heads, float32: 73.4 us without, 70.7 us with). FULL: head_dim is DP.
+// W, so that a product takes several parts at a time. FULL: head_dim is DP.
 // STREAM: past the caches, as no other workgroup reads the same rows.
 template <int XT, int DP, int NT, int W, bool FULL, bool STREAM>
 __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2m1_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
@@ -628,7 +627,16 @@ void launch_kernel(const AttendLaunch& a, const Work& w, const Plan& p, hipStrea
 template <int XT, int DP, bool FULL>
 void launch_tiles(const AttendLaunch& a, const Work& w, const Plan& p, hipStream_t s) {
   const int32_t group = a.heads / a.c.kv_heads;
-  if constexpr (FULL) {
+  // Parts side by side, 64 sequences and 8 key/value heads, without and with, us:
+  //   heads of                 128         96        64        256 (up to 4096 tokens)
+  //   float32, groups of 4  71.5, 64.5  74.6, 69.4  52.6, 50.4  101.0, 92.6
+  //   float32, groups of 8  75.5, 74.4  75.1, 72.9  54.1, 52.9  106.0, 102.3
+  //   f16, groups of 4      62.3, 59.5  63.4, 59.3  45.8, 44.5  85.9, 83.4
+  //   f16, groups of 8      64.6, 62.2  64.6, 61.1  47.8, 47.3  90.2, 87.1
+  //   bf16, groups of 4     59.4, 59.2  56.6, 55.8  42.3, 41.3  78.5, 81.3
+  //   bf16, groups of 8     61.7, 61.5  57.9, 58.8  44.5, 43.3  82.2, 83.8
+  // (a bf16 query is one part: only its weights' two are taken together).
+  if constexpr (DP < 256 || Form<XT, DP>::kParts > 1) {
     if (group <= 4) return launch_kernel<XT, DP, 1, 4, FULL, true>(a, w, p, s);
     if (group <= 8) return launch_kernel<XT, DP, 1, 8, FULL, true>(a, w, p, s);
   }
