@@ -12,16 +12,7 @@ namespace {
 constexpr int kWaves = 4;                 // per workgroup
 constexpr int kHeadTile = 16;
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-// The buffer a page's rows of one head are read through: a load past `bytes`
-// gives zeros.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, bytes, 0x00020000);
-}
-constexpr int kNowhere = 0x40000000;      // an offset past every page
-constexpr int kStream = 2;                // cache policy: read once, not to be kept
 
 // max or sum over the four lanes of a head (lane mod 16)
 __device__ __forceinline__ float head_max(float v) {
@@ -48,16 +39,6 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// x as the sum of PARTS 16-bit numbers, each rounded from what the ones before leave.
-template <class T, int PARTS>
-__device__ __forceinline__ void split(float x, T* part) {
-#pragma unroll
-  for (int s = 0; s < PARTS; ++s) {
-    part[s] = (T)x;
-    x -= (float)part[s];
-  }
-}
 
 // Tokens are dealt out in steps of kStepTokens (a sequence's last one may be
 // short). With `total` steps of all sequences, workgroup u of a key/value head

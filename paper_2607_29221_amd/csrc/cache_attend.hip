@@ -41,7 +41,26 @@
 namespace mosaic {
 namespace {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// The buffer a page's rows of one head are read through: a load past `bytes`
+// gives zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, bytes, 0x00020000);
+}
+constexpr int kNowhere = 0x40000000;      // an offset past every page
+constexpr int kStream = 2;                // cache policy: read once, not to be kept
+
+// x as the sum of PARTS 16-bit numbers, each rounded from what the ones before leave.
+template <class T, int PARTS>
+__device__ __forceinline__ void split(float x, T* part) {
+#pragma unroll
+  for (int s = 0; s < PARTS; ++s) {
+    part[s] = (T)x;
+    x -= (float)part[s];
+  }
+}
 
 // What the types of cache and activations make of a wave's step. DP: head_dim
 // padded to 64, 128 or 256 (columns beyond head_dim are zeros).
