@@ -23,11 +23,11 @@
 //   permutes once they are bf16.
 //
 // Measured on an MI355X with the join, heads of 128 elements: 131072 tokens of one
-// sequence, 32 query and 8 key/value heads, bf16, 35 us, 27 to 31 us in this kernel
-// (168 MB: 5.4 to 6.2 TB/s); 64 sequences of 512 to 7168 tokens, 64 and 8 heads,
-// bf16 62 us, float32 71 to 75 us (315 MB: 5.8 and 4.9 TB/s in this kernel). What is
-// left above the bandwidth: with the loads alone the 64 sequences take 61 us, with
-// the arithmetic alone 65 (before parts lay side by side); a part of a sequence
+// sequence, 32 query and 8 key/value heads, bf16, 35 us, 29 to 31 us in this kernel
+// (168 MB: 5.4 to 5.8 TB/s); 64 sequences of 512 to 7168 tokens, 64 and 8 heads,
+// bf16 61 us, float32 67 to 75 us (315 MB: 5.6 and 4.5 to 4.8 TB/s in this kernel).
+// What is left above the bandwidth: without the arithmetic the 64 sequences (float32)
+// take 62 of 75 us, without the rows past a part's first steps 68; a part of a sequence
 // starts with 3.5 to 5.5 us of dependent loads, and about 200 vector instructions
 // per 32 tokens and wave leave the two waves of a SIMD little room.
 #include <cfloat>
@@ -88,7 +88,7 @@ template <int N> __device__ __forceinline__ void landed() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-constexpr int waves_of(int DP, int NT) { return DP == 256 ? 1 : 2; }
+constexpr int waves_of(int DP) { return DP == 256 ? 1 : 2; }
 
 // Weights as bf16 parts, two to a dword.
 template <int PARTS> __device__ __forceinline__ void split_pair(float x, float y, uint32_t* part) {
@@ -140,7 +140,7 @@ template <int XT, int DP> bool two_fit(const AttendLaunch& a) {
 // W, so that a product takes several parts at a time. FULL: head_dim is DP.
 // STREAM: past the caches, as no other workgroup reads the same rows.
 template <int XT, int DP, int NT, int W, bool FULL, bool STREAM>
-__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NT)) void cache_attend_e2m1_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP)) void cache_attend_e2m1_kernel(AttendLaunch a, Work wk, int32_t workgroups) {
   typedef Form<XT, DP> F;
   typedef Lds<XT, DP, NT, W> S;
   typedef typename F::X X;
