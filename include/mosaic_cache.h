@@ -32,6 +32,9 @@
  * a cache in 4 bits, in bytes).
  * Both orders, (page, head, place) and (page, place, head), and gaps are
  * fine, as long as the rows of a page do not overlap and pages do not.
+ * head_stride (of several heads) is 2^19 - 1 at most, so that pages of 4096
+ * places by heads have rows below 128 elements (in 4 bits, bytes); token_stride
+ * is 2^27 / page_size at most.
  * Alongside every row two numbers may be kept, in contiguous arrays of
  * pages x kv_heads x page_size: ``weights``, the attention weight that the
  * token has got from the queries of this head's group so far, and ``order``,
